@@ -241,6 +241,132 @@ int unstep_step(unstep_cache* c, int32_t start_frame, int32_t n_frames, int32_t 
                 float softmax_scale, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* ---------------------------------------------------------------------------------
+ * Rotary options: how a head's pairs are split over the axes, which layout they have, how much of
+ * the head they cover, and the scaling of the frame axis for clips longer than the trained ones.
+ * ------------------------------------------------------------------------------- */
+
+/* Scaling of the frame axis (its angle per frame w_k, k = 0 .. dim_t/2 - 1, s = factor >= 1):
+ *   UNSCALED  w_k = theta^(-2k/dim_t)
+ *   LINEAR    w_k / s: positions interpolated into the trained range
+ *   BASE      theta' = theta s^(dim_t/(dim_t-2)): the slowest pair turns by 1/s, the fastest as trained
+ *   PARTS     w_k (g_k + (1 - g_k)/s), g_k = clamp((n_k - turns_slow)/(turns_fast - turns_slow), 0, 1),
+ *             n_k = trained_frames w_k / 2 pi the turns of pair k over the trained length: fast pairs
+ *             keep their angle, slow ones are interpolated, a ramp in between */
+typedef enum {
+  UNSTEP_ROTARY_UNSCALED = 0,
+  UNSTEP_ROTARY_LINEAR = 1,
+  UNSTEP_ROTARY_BASE = 2,
+  UNSTEP_ROTARY_PARTS = 3
+} unstep_rotary_scaling;
+
+/* Pair j of the rotated part of a head (rot_dim dimensions from the first on; the others are left as
+ * they are): INTERLEAVED (x[2j], x[2j+1]), HALF (x[j], x[j + rot_dim/2]). */
+typedef enum { UNSTEP_ROTARY_INTERLEAVED = 0, UNSTEP_ROTARY_HALF = 1 } unstep_rotary_layout;
+
+typedef struct {
+  int32_t dim_t, dim_h, dim_w;   /* dimensions turned by the frame, the grid row and the grid column, in
+                                    that order: even, their sum (rot_dim) a multiple of 16 up to 128 */
+  int32_t scaling;               /* an unstep_rotary_scaling */
+  double theta;                  /* > 1 */
+  double factor;                 /* s above; ignored when UNSCALED */
+  double trained_frames;         /* PARTS only: trained length in frames, > 0 */
+  double turns_fast, turns_slow; /* PARTS only: 0 <= turns_slow < turns_fast (32 and 1 are usual) */
+  double amplitude;              /* factor of both tables; 0: 1, for PARTS 0.1 ln(s) + 1 */
+} unstep_rotary;
+
+/* Tables cos_out, sin_out (device float [N, rot_dim/2]) of the chunk [start_frame, start_frame +
+ * n_frames): amplitude times cos and sin of the token's absolute frame index, row or column times the
+ * pair's angle, evaluated in double precision and rounded once to float.  One launch on hip_stream: no
+ * upload, no synchronisation, so it can be captured in a graph.  With dims (44, 42, 42) unscaled they are the
+ * tables of unstep_rope_tables (within one float rounding: the device's cos and sin may differ from the C
+ * library's in the last bit of the double).  Errors: E_NULL, E_SHAPE (sizes < 1, dims, more than 2^23
+ * tokens), E_RANGE (start_frame < 0, theta, scaling, factor < 1, trained_frames, turns, amplitude < 0 or not
+ * finite), E_ALIGN, E_HIP. */
+int unstep_rotary_tables(int32_t start_frame, int32_t n_frames, int32_t grid_h, int32_t grid_w,
+                         const unstep_rotary* rotary, float* cos_out, float* sin_out, void* hip_stream);
+
+/* unstep_kv_append with the rotation's options and, when k_norm_weight is not NULL, the normalisation of
+ * unstep_kv_append_qknorm.  layout: an unstep_rotary_layout; cos_t, sin_t: device float [N, rot_dim/2].
+ * y_a = x_a*c - x_b*s, y_b = x_a*s + x_b*c with the rounding contract of unstep_kv_append; dimensions
+ * from rot_dim on are copied.  INTERLEAVED with rot_dim 128 is unstep_kv_append (or _qknorm) bit for bit.
+ * q, k, v, strides, q_rot, index update: as there.  Errors: those of unstep_kv_append (with
+ * weights, of unstep_kv_append_qknorm), plus E_SHAPE (rot_dim no multiple of 16 in [16, 128]; N * n_heads
+ * above 2^27 - 1), E_RANGE (layout), E_STATE (the cache holds quantised rows). */
+int unstep_kv_append_rotary(unstep_cache* c, int32_t start_frame, int32_t n_frames,
+                            const void* q, const void* k, const void* v,
+                            int64_t tok_stride, int64_t head_stride,
+                            const float* cos_t, const float* sin_t, int32_t layout, int32_t rot_dim,
+                            const void* q_norm_weight, const void* k_norm_weight, double norm_eps,
+                            void* q_rot, void* hip_stream);
+
+/* ---------------------------------------------------------------------------------
+ * Quantised KV cache: half the bytes of the bf16 one, and a faster product with the queries.
+ *
+ * A row of 128 values is four blocks of 32, each held as e4m3 values (8 bits: sign, 4 exponent bits, 3
+ * fraction bits, at most 448, no infinity) times one power of two 2^(byte - 127).  For values y the block's
+ * exponent e = byte - 127 is the smallest integer >= -100 with max|y| * 2^-e <= 448, and the held value is
+ * y * 2^-e rounded to e4m3 (nearest even), off by at most half a step.  A value that is not finite is
+ * held as NaN and does not count towards the maximum.  Held values are exact in bf16 (one that rounds up to
+ * 2^128, from |y| >= 248 * 2^120 on, reads back as infinity).
+ * ------------------------------------------------------------------------------- */
+
+/* A handle over caller-owned device buffers k8, v8 (e4m3 bytes [batch, n_heads, slots, 128]) and k_scale,
+ * v_scale (bytes [batch, n_heads, slots, 4]), slots = (sink_frames + ring_frames) * grid_h * grid_w, all
+ * 16-byte aligned.  The index calls (frame_map, advance, window_segments, attn_workspace_size, destroy) are
+ * the same for both kinds of handle; the calls that touch rows refuse the other kind (E_STATE).
+ * Errors: as unstep_cache_create. */
+int unstep_cache_create_mx8(unstep_cache** out, int32_t batch, int32_t n_heads, int32_t head_dim,
+                            int32_t grid_h, int32_t grid_w, int32_t sink_frames, int32_t ring_frames,
+                            void* k8, void* k_scale, void* v8, void* v_scale);
+
+/* unstep_kv_append_rotary into a quantised cache.  The rotated keys and the values are quantised from their
+ * float values (no bf16 rounding in between).  The queries are multiplied by float(softmax_scale * log2 e)
+ * (a float product; softmax_scale <= 0 selects 1/sqrt(128)) and quantised too, into q8 (e4m3
+ * [batch, N, n_heads, 128]) and q_scale (bytes [batch, N, n_heads, 4], 4-byte aligned): the attention then
+ * needs no factor per score, its weights are 2^(q.k).  Errors: those of unstep_kv_append_rotary, plus
+ * E_NULL (q8 or q_scale when q != NULL), E_RANGE (softmax_scale not finite), E_STATE (the cache holds bf16
+ * rows). */
+int unstep_kv_append_mx8(unstep_cache* c, int32_t start_frame, int32_t n_frames,
+                         const void* q, const void* k, const void* v,
+                         int64_t tok_stride, int64_t head_stride,
+                         const float* cos_t, const float* sin_t, int32_t layout, int32_t rot_dim,
+                         const void* q_norm_weight, const void* k_norm_weight, double norm_eps,
+                         float softmax_scale, void* q8, void* q_scale, void* hip_stream);
+
+/* unstep_window_attn over a quantised cache: out = sum_m 2^(q.k_m) v_m / sum_m 2^(q.k_m) over the retained
+ * keys, for q8, q_scale as unstep_kv_append_mx8 writes them.  Products of e4m3 values with fp32
+ * accumulation (the matrix instruction cuts a product below 2^-13 of the largest of its 16 dimensions, so
+ * a score that one product of size P dominates is off by up to 2^-8 P), fp32 softmax, probabilities rounded to bf16 for their product with the values; out is bf16
+ * [batch, N, n_heads, 128], lse (optional) float [batch, n_heads, N], the natural logarithm of the sum.
+ * Scale bytes must lie in [1, 254].  Workspace: as unstep_window_attn, of unstep_attn_workspace_size bytes
+ * for this handle.  Errors: those of unstep_window_attn, plus E_NULL (q_scale), E_STATE (the cache holds bf16 rows). */
+int unstep_window_attn_mx8(const unstep_cache* c, int32_t start_frame, int32_t n_frames,
+                           int32_t window_frames, const void* q8, const void* q_scale, void* out, float* lse,
+                           void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* One whole chunk step on a quantised cache: unstep_kv_append_mx8 followed by unstep_window_attn_mx8 on the
+ * same stream (q must not be NULL).  All checks of both halves run before anything is enqueued.  Errors:
+ * the union of both. */
+int unstep_step_mx8(unstep_cache* c, int32_t start_frame, int32_t n_frames, int32_t window_frames,
+                    const void* q, const void* k, const void* v, int64_t tok_stride, int64_t head_stride,
+                    const float* cos_t, const float* sin_t, int32_t layout, int32_t rot_dim,
+                    const void* q_norm_weight, const void* k_norm_weight, double norm_eps, float softmax_scale,
+                    void* q8, void* q_scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                    void* hip_stream);
+
+/* The frames [start_frame, start_frame + n_frames) of a quantised cache read back: k_out, v_out bf16
+ * [batch, N, n_heads, 128] (the layout of unstep_kv_append's inputs; the keys rotated), exact.
+ * Errors: E_NULL, E_SHAPE (n_frames < 1, more than 2^27 head rows), E_RANGE (start_frame < 0), E_STATE (a frame
+ * is not in the cache; the cache holds bf16 rows), E_ALIGN, E_HIP. */
+int unstep_kv_read_mx8(const unstep_cache* c, int32_t start_frame, int32_t n_frames, void* k_out, void* v_out,
+                       void* hip_stream);
+
+/* out = the bf16 values of `rows` quantised rows: x8 e4m3 [rows, 128], scale bytes [rows, 4], out bf16
+ * [rows, 128], contiguous (scale of any alignment).  Errors: E_NULL, E_SHAPE (rows outside [0, 2^27]),
+ * E_ALIGN, E_HIP. */
+int unstep_mx8_dequantize(const void* x8, const void* scale, void* out, int64_t rows, void* hip_stream);
+
+/* ---------------------------------------------------------------------------------
  * Sampler schedule and clean-cache updates (Section 3.4, Equations 1 and 3, and the
  * appendix's shift-five schedule; a later row than the attention step).
  * ------------------------------------------------------------------------------- */

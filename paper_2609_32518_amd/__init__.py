@@ -10,7 +10,8 @@ PyTorch provides device memory (tensors) and the stream; the library's C ABI
 ``unstep_rope_tables``, ``unstep_kv_append`` (+ ``_qknorm``), ``unstep_window_attn``, ``unstep_step``
 as methods of a ``Cache`` handle (or functions), ``RopeTableCache`` for the per-chunk tables, and
 the clip-level calls ``unstep_sampler_calls``, ``unstep_shift_schedule``, ``unstep_renoise``,
-``unstep_emit``, ``unstep_svd_truncate`` and ``unstep_linear``.
+``unstep_emit``, ``unstep_svd_truncate`` and ``unstep_linear``.  ``rotary`` holds the rotary options
+(tables, layouts), ``mx8`` the quantised cache (``CacheMX8``).
 
 Importing this package loads libunstep.so and raises if it is missing: there is no
 fallback path.  Build it with ``python paper_2609_32518_amd/build.py``.
@@ -76,6 +77,18 @@ SIGNATURES = {
     "unstep_window_attn_noalloc": (ctypes.c_int, [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _f32, _vp]),
     "unstep_step": (ctypes.c_int, [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _vp,
                                    _f32, _vp, _sz, _vp]),
+    "unstep_rotary_tables": (ctypes.c_int, [_i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp]),
+    "unstep_kv_append_rotary": (ctypes.c_int, [_vp, _i32, _i32, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _i32, _i32, _vp,
+                                               _vp, _f64, _vp, _vp]),
+    "unstep_cache_create_mx8": (ctypes.c_int, [ctypes.POINTER(_vp), _i32, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp,
+                                               _vp, _vp]),
+    "unstep_kv_append_mx8": (ctypes.c_int, [_vp, _i32, _i32, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _i32, _i32, _vp, _vp,
+                                            _f64, _f32, _vp, _vp, _vp]),
+    "unstep_window_attn_mx8": (ctypes.c_int, [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "unstep_step_mx8": (ctypes.c_int, [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _i32, _i32, _vp, _vp,
+                                       _f64, _f32, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "unstep_kv_read_mx8": (ctypes.c_int, [_vp, _i32, _i32, _vp, _vp, _vp]),
+    "unstep_mx8_dequantize": (ctypes.c_int, [_vp, _vp, _vp, _i64, _vp]),
 }
 for _name, (_res, _args) in SIGNATURES.items():
     _fn = getattr(lib, _name)
@@ -337,6 +350,16 @@ class Cache:
         _used_on(stream, q_rot)
         return q_rot
 
+    def unstep_kv_append_rotary(self, start_frame: int, n_frames: int, q: Optional[torch.Tensor], k: torch.Tensor,
+                                v: torch.Tensor, cos_t: torch.Tensor, sin_t: torch.Tensor,
+                                layout: str = "interleaved", q_norm_weight: Optional[torch.Tensor] = None,
+                                k_norm_weight: Optional[torch.Tensor] = None, norm_eps: float = 1e-6,
+                                q_rot: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+        """unstep_kv_append with pairs in either layout over the first rot_dim dimensions of a head
+        (tables [N, rot_dim / 2]) and, with weights, the normalisation of unstep_kv_append_qknorm."""
+        return rotary.append_rotary(self, start_frame, n_frames, q, k, v, cos_t, sin_t, layout, q_norm_weight,
+                                    k_norm_weight, norm_eps, q_rot, stream)
+
     def unstep_window_attn(self, start_frame: int, n_frames: int, window_frames: int, q_rot: torch.Tensor,
                            out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
                            softmax_scale: float = 0.0, workspace: Optional[torch.Tensor] = None,
@@ -556,3 +579,8 @@ def unstep_mfma_reference(src: torch.Tensor, groups: int, waves_per_simd: int, m
     _check(lib.unstep_mfma_reference(src.data_ptr(), out.data_ptr(), groups, waves_per_simd, mfmas, _stream(stream)))
     _used_on(stream, src, out)
     return out
+
+
+from . import rotary  # noqa: E402
+from .rotary import ROTARY_LAYOUTS, ROTARY_SCALINGS, unstep_rotary_tables  # noqa: E402,F401
+from .mx8 import CacheMX8, unstep_mx8_dequantize  # noqa: E402,F401

@@ -6,32 +6,29 @@
 // unstep_rope_tables, which waits for its table upload.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <string>
 #include <vector>
 
-#include "cache_index.hpp"
 #include "kernels.hpp"
+#include "plan.hpp"
 #include "rope_tables.hpp"
 #include "status.hpp"
 #include "unstep.h"
 
-struct unstep_cache {
-  unstep::CacheIndex idx;
-  int32_t B, H, D, grid_h, grid_w;
-  int32_t slots;
-  uint16_t* k;
-  uint16_t* v;
-};
-
 namespace {
 
 using unstep::aligned16;
+using unstep::AppendPlan;
 using unstep::fail;
 using unstep::fail_msg;
+using unstep::need_kind;
 using unstep::ok;
+using unstep::plan_append;
+using unstep::plan_attn;
 
 int check_table_args(const char* where, int32_t f0, int32_t F, int32_t gh, int32_t gw, int32_t D,
                      double theta, const void* c, const void* s) {
@@ -42,110 +39,6 @@ int check_table_args(const char* where, int32_t f0, int32_t F, int32_t gh, int32
     return fail(UNSTEP_E_SHAPE, "%s: table too large", where);
   if (f0 < 0 || int64_t(f0) + F > INT32_MAX) return fail(UNSTEP_E_RANGE, "%s: bad start_frame", where);
   if (!(theta > 1.0) || !std::isfinite(theta)) return fail(UNSTEP_E_RANGE, "%s: theta must be > 1", where);
-  return UNSTEP_OK;
-}
-
-struct AppendPlan {
-  unstep::RopeAppendArgs args;
-};
-
-// Validation of an append on index `idx` (which may be a scratch copy).
-int plan_append(const unstep_cache* c, const unstep::CacheIndex& idx, int32_t f0, int32_t C,
-                const void* q, const void* k, const void* v, int64_t tok_stride, int64_t head_stride,
-                const float* cos_t, const float* sin_t, void* q_rot, AppendPlan* plan, const char* where) {
-  if (!c) return fail(UNSTEP_E_NULL, "%s: cache handle is NULL", where);
-  if (!k || !v || !cos_t || !sin_t) return fail(UNSTEP_E_NULL, "%s: k, v, cos_t or sin_t is NULL", where);
-  if (q && !q_rot) return fail(UNSTEP_E_NULL, "%s: q given but q_rot is NULL", where);
-  std::string why;
-  int rc = idx.check_append(f0, C, &why);
-  if (rc != UNSTEP_OK) return fail_msg(rc, where, why);
-  if (head_stride < UNSTEP_HEAD_DIM || tok_stride < int64_t(c->H) * head_stride)
-    return fail(UNSTEP_E_SHAPE, "%s: strides (tok %lld, head %lld) overlap for %d heads of 128", where,
-                (long long)tok_stride, (long long)head_stride, c->H);
-  if ((tok_stride % 8) || (head_stride % 8))
-    return fail(UNSTEP_E_ALIGN, "%s: strides must be multiples of 8 elements", where);
-  if (!aligned16(k) || !aligned16(v) || !aligned16(cos_t) || !aligned16(sin_t) || (q && !aligned16(q)) ||
-      (q_rot && !aligned16(q_rot)))
-    return fail(UNSTEP_E_ALIGN, "%s: pointers must be 16-byte aligned", where);
-  unstep::RopeAppendArgs& a = plan->args;
-  a.q = static_cast<const uint16_t*>(q);
-  a.k = static_cast<const uint16_t*>(k);
-  a.v = static_cast<const uint16_t*>(v);
-  a.tok_stride = tok_stride;
-  a.head_stride = head_stride;
-  a.cos_t = cos_t;
-  a.sin_t = sin_t;
-  a.q_rot = q ? static_cast<uint16_t*>(q_rot) : nullptr;
-  a.k_cache = c->k;
-  a.v_cache = c->v;
-  a.B = c->B;
-  a.H = c->H;
-  a.T = idx.T();
-  a.C = C;
-  a.slots = c->slots;
-  a.f0 = f0;
-  a.S = idx.S();
-  a.R = idx.R();
-  a.wq = nullptr;
-  a.wk = nullptr;
-  a.eps = 0.0;
-  return UNSTEP_OK;
-}
-
-int plan_attn(const unstep_cache* c, const unstep::CacheIndex& idx, int32_t f0, int32_t C, int32_t W,
-              const void* q_rot, void* out, float* lse, float scale, void* workspace, size_t ws_bytes,
-              unstep::AttnArgs* a, const char* where) {
-  if (!c) return fail(UNSTEP_E_NULL, "%s: cache handle is NULL", where);
-  if (!q_rot || !out) return fail(UNSTEP_E_NULL, "%s: q_rot or out is NULL", where);
-  unstep::Segments logical;
-  std::string why;
-  int rc = idx.segments(f0, C, W, &logical, &why);
-  if (rc != UNSTEP_OK) return fail_msg(rc, where, why);
-  const unstep::Segments seg = unstep::cache_order(logical);
-  if (!aligned16(q_rot) || !aligned16(out) || (lse && (reinterpret_cast<uintptr_t>(lse) & 3u)) ||
-      (workspace && !aligned16(workspace)))
-    return fail(UNSTEP_E_ALIGN, "%s: pointers must be 16-byte aligned", where);
-  const int32_t N = C * idx.T();
-  // one 512-thread work-group per 256-query tile: the launch's work-item count must fit 32 bits
-  if (int64_t(c->B) * c->H * ((int64_t(N) + 255) / 256) * 512 > int64_t(UINT32_MAX))
-    return fail(UNSTEP_E_SHAPE, "%s: too many query tiles (batch x heads x chunk tokens / 256 >= 2^23)", where);
-  a->q = static_cast<const uint16_t*>(q_rot);
-  a->k_cache = c->k;
-  a->v_cache = c->v;
-  a->out = static_cast<uint16_t*>(out);
-  a->lse = lse;
-  a->B = c->B;
-  a->N = N;
-  a->H = c->H;
-  a->slots = c->slots;
-  a->n_keys = seg.total();
-  a->n_seg = seg.n;
-  int32_t l = 0;
-  for (int i = 0; i < UNSTEP_MAX_SEGMENTS; ++i) {
-    if (i < seg.n) {
-      a->seg_l0[i] = l;
-      a->seg_row0[i] = seg.row0[i];
-      l += seg.len[i];
-    } else {
-      a->seg_l0[i] = INT32_MAX;
-      a->seg_row0[i] = 0;
-    }
-  }
-  a->seg_l0[UNSTEP_MAX_SEGMENTS] = INT32_MAX;
-  a->scale = scale > 0.f ? scale : 1.0f / std::sqrt(float(UNSTEP_HEAD_DIM));
-  const unstep::AttnPlan plan = unstep::attn_plan(c->B, c->H, N, a->n_keys, workspace ? ws_bytes : 0);
-  a->parts = 1;
-  if (plan.workspace > 0) {
-    a->groups = plan.groups;
-    a->parts = plan.parts;
-    a->part_o = static_cast<float*>(workspace);
-    a->part_ml = static_cast<float*>(workspace) + plan.part_o_floats;
-  } else {
-    // one work-group per query tile over the whole key range: no scratch needed
-    a->groups = plan.plain_groups;
-    a->part_o = nullptr;
-    a->part_ml = nullptr;
-  }
   return UNSTEP_OK;
 }
 
@@ -176,8 +69,7 @@ int unstep_cache_create(unstep_cache** out, int32_t batch, int32_t n_heads, int3
       return fail(UNSTEP_E_ALIGN, "unstep_cache_create: cache buffers must be 16-byte aligned");
     unstep_cache* c = new (std::nothrow) unstep_cache{unstep::CacheIndex(int32_t(T), sink_frames, ring_frames),
                                                       batch, n_heads, head_dim, grid_h, grid_w, int32_t(slots),
-                                                      static_cast<uint16_t*>(k_cache),
-                                                      static_cast<uint16_t*>(v_cache)};
+                                                      k_cache, v_cache, nullptr, nullptr};
     if (!c) return fail(UNSTEP_E_HOST, "unstep_cache_create: out of host memory");
     *out = c;
     return ok();
@@ -262,9 +154,9 @@ int unstep_kv_append(unstep_cache* c, int32_t start_frame, int32_t n_frames, con
                      const void* v, int64_t tok_stride, int64_t head_stride, const float* cos_t,
                      const float* sin_t, void* q_rot, void* hip_stream) {
   return unstep::guarded("unstep_kv_append", [&]() -> int {
-    if (!c) return fail(UNSTEP_E_NULL, "unstep_kv_append: cache handle is NULL");
+    if (int rc = need_kind(c, false, "unstep_kv_append")) return rc;
     AppendPlan p;
-    int rc = plan_append(c, c->idx, start_frame, n_frames, q, k, v, tok_stride, head_stride, cos_t, sin_t, q_rot,
+    int rc = plan_append(c, start_frame, n_frames, q, k, v, tok_stride, head_stride, cos_t, sin_t, q_rot,
                          &p, "unstep_kv_append");
     if (rc != UNSTEP_OK) return rc;
     hipError_t e = unstep::launch_rope_append(p.args, static_cast<hipStream_t>(hip_stream));
@@ -280,7 +172,7 @@ int unstep_kv_append_qknorm(unstep_cache* c, int32_t start_frame, int32_t n_fram
                             double norm_eps, void* q_rot, void* hip_stream) {
   return unstep::guarded("unstep_kv_append_qknorm", [&]() -> int {
     const char* where = "unstep_kv_append_qknorm";
-    if (!c) return fail(UNSTEP_E_NULL, "%s: cache handle is NULL", where);
+    if (int rc = need_kind(c, false, where)) return rc;
     if (!k_norm_weight || (q && !q_norm_weight))
       return fail(UNSTEP_E_NULL, "%s: k_norm_weight (and q_norm_weight when q is given) is NULL", where);
     if (c->H > unstep::kNormMaxHeads)
@@ -289,7 +181,7 @@ int unstep_kv_append_qknorm(unstep_cache* c, int32_t start_frame, int32_t n_fram
     if (!(norm_eps >= 0.0) || !std::isfinite(norm_eps))
       return fail(UNSTEP_E_RANGE, "%s: norm_eps must be finite and >= 0", where);
     AppendPlan p;
-    int rc = plan_append(c, c->idx, start_frame, n_frames, q, k, v, tok_stride, head_stride, cos_t, sin_t, q_rot,
+    int rc = plan_append(c, start_frame, n_frames, q, k, v, tok_stride, head_stride, cos_t, sin_t, q_rot,
                          &p, where);
     if (rc != UNSTEP_OK) return rc;
     if (!aligned16(k_norm_weight) || (q && !aligned16(q_norm_weight)))
@@ -322,9 +214,9 @@ int unstep_window_attn(const unstep_cache* c, int32_t start_frame, int32_t n_fra
                        const void* q_rot, void* out, float* lse, float softmax_scale, void* workspace,
                        size_t workspace_bytes, void* hip_stream) {
   return unstep::guarded("unstep_window_attn", [&]() -> int {
-    if (!c) return fail(UNSTEP_E_NULL, "unstep_window_attn: cache handle is NULL");
+    if (int rc = need_kind(c, false, "unstep_window_attn")) return rc;
     unstep::AttnArgs a;
-    int rc = plan_attn(c, c->idx, start_frame, n_frames, window_frames, q_rot, out, lse, softmax_scale, workspace,
+    int rc = plan_attn(c, c->idx.newest(), start_frame, n_frames, window_frames, q_rot, out, lse, softmax_scale, workspace,
                        workspace_bytes, &a, "unstep_window_attn");
     if (rc != UNSTEP_OK) return rc;
     hipError_t e = unstep::launch_window_attn(a, static_cast<hipStream_t>(hip_stream));
@@ -337,9 +229,9 @@ int unstep_window_attn_noalloc(const unstep_cache* c, int32_t start_frame, int32
                                const void* q_rot, void* out, float* lse, float softmax_scale, void* hip_stream) {
   return unstep::guarded("unstep_window_attn_noalloc", [&]() -> int {
     const char* where = "unstep_window_attn_noalloc";
-    if (!c) return fail(UNSTEP_E_NULL, "%s: cache handle is NULL", where);
+    if (int rc = need_kind(c, false, where)) return rc;
     unstep::AttnArgs a;
-    int rc = plan_attn(c, c->idx, start_frame, n_frames, window_frames, q_rot, out, lse, softmax_scale, nullptr, 0,
+    int rc = plan_attn(c, c->idx.newest(), start_frame, n_frames, window_frames, q_rot, out, lse, softmax_scale, nullptr, 0,
                        &a, where);
     if (rc != UNSTEP_OK) return rc;
     const unstep::AttnPlan plan = unstep::attn_plan(a.B, a.H, a.N, a.n_keys);
@@ -368,22 +260,22 @@ int unstep_step(unstep_cache* c, int32_t start_frame, int32_t n_frames, int32_t 
                 const float* sin_t, void* q_rot, void* out, float* lse, float softmax_scale, void* workspace,
                 size_t workspace_bytes, void* hip_stream) {
   return unstep::guarded("unstep_step", [&]() -> int {
-    if (!c) return fail(UNSTEP_E_NULL, "unstep_step: cache handle is NULL");
+    if (int rc = need_kind(c, false, "unstep_step")) return rc;
     if (!q) return fail(UNSTEP_E_NULL, "unstep_step: q is NULL");
     AppendPlan p;
-    int rc = plan_append(c, c->idx, start_frame, n_frames, q, k, v, tok_stride, head_stride, cos_t, sin_t, q_rot, &p,
+    int rc = plan_append(c, start_frame, n_frames, q, k, v, tok_stride, head_stride, cos_t, sin_t, q_rot, &p,
                          "unstep_step");
     if (rc != UNSTEP_OK) return rc;
-    unstep::CacheIndex after = c->idx;      // the attention half is checked on the post-append state
-    after.commit_append(start_frame, n_frames);
+    // the attention half is checked on the post-append state
+    const int32_t newest = std::max(c->idx.newest(), start_frame + n_frames - 1);
     unstep::AttnArgs a;
-    rc = plan_attn(c, after, start_frame, n_frames, window_frames, q_rot, out, lse, softmax_scale, workspace,
+    rc = plan_attn(c, newest, start_frame, n_frames, window_frames, q_rot, out, lse, softmax_scale, workspace,
                    workspace_bytes, &a, "unstep_step");
     if (rc != UNSTEP_OK) return rc;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     hipError_t e = unstep::launch_rope_append(p.args, st);
     if (e != hipSuccess) return fail(UNSTEP_E_HIP, "unstep_step (append): %s", hipGetErrorString(e));
-    c->idx = after;
+    c->idx.commit_append(start_frame, n_frames);
     e = unstep::launch_window_attn(a, st);
     if (e != hipSuccess) return fail(UNSTEP_E_HIP, "unstep_step (attention): %s", hipGetErrorString(e));
     return ok();

@@ -8,6 +8,7 @@
 // lo = max(0, f0 - W).
 #pragma once
 
+#include <algorithm>
 #include <cstdint>
 #include <string>
 #include <utility>
@@ -94,22 +95,14 @@ class CacheIndex {
     if (f0 + C - 1 > newest_) newest_ = f0 + C - 1;
   }
 
-  // Retained frames in logical order (sinks, window, chunk), validated.
-  int retained(int32_t f0, int32_t C, int32_t W, std::vector<int32_t>* frames, std::string* why) const {
-    if (C < 1) return fail(UNSTEP_E_SHAPE, "empty chunk (n_frames < 1)", why);
-    if (f0 < 0 || W < 0) return fail(UNSTEP_E_RANGE, "negative start frame or window", why);
-    if (int64_t(f0) + C - 1 > INT32_MAX - 1) return fail(UNSTEP_E_RANGE, "frame index overflow", why);
-    const int32_t lo = f0 - W > 0 ? f0 - W : 0;
-    const int32_t n_sink = S_ < lo ? S_ : lo;
-    // the sinks lie below S; the window and the chunk may not need more ring slots than exist
-    if (ring_count(lo, int64_t(f0) + C) > R_)
-      return fail(UNSTEP_E_RANGE, "window plus chunk has more ring frames than the ring holds", why);
-    frames->clear();
-    for (int32_t f = 0; f < n_sink; ++f) frames->push_back(f);
-    for (int32_t f = lo; f < f0 + C; ++f) frames->push_back(f);
-    for (int32_t f : *frames)
-      if (!resident(f)) return fail(UNSTEP_E_STATE, "frame " + std::to_string(f) + " is not in the cache", why);
-    return UNSTEP_OK;
+  // First frame of [a, b) that is not in the cache once `newest` is the newest stored, or b.  Appends leave no
+  // gap and each new ring frame evicts the one R before it, so the cache holds the sinks up to `newest`
+  // and the last R ring frames: the answer takes no walk over the frames (a single-token stream's window
+  // holds tens of thousands).
+  int32_t first_missing(int32_t a, int32_t b, int32_t newest) const {
+    const int32_t ring = a > S_ ? a : S_;              // the range's first ring frame
+    if (ring < b && ring <= newest && ring <= int64_t(newest) - R_) return a < S_ && newest + 1 < S_ ? std::max(a, newest + 1) : ring;
+    return std::min(b, std::max(a, newest + 1));
   }
 
   // Number of retained frames from the window formula alone (no residency check; the ring
@@ -125,22 +118,39 @@ class CacheIndex {
     return UNSTEP_OK;
   }
 
-  // Retained keys as maximal runs of consecutive cache rows, in logical order.
+  // Retained keys as maximal runs of consecutive cache rows, in logical order (sinks, window, chunk).
   int segments(int32_t f0, int32_t C, int32_t W, Segments* out, std::string* why) const {
-    std::vector<int32_t> frames;
-    int rc = retained(f0, C, W, &frames, why);
+    return segments(f0, C, W, newest_, out, why);
+  }
+  // The same with `newest` as the newest stored frame: after an append that reaches it.
+  int segments(int32_t f0, int32_t C, int32_t W, int32_t newest, Segments* out, std::string* why) const {
+    int32_t count = 0;
+    const int rc = retained_count(f0, C, W, &count, why);
     if (rc != UNSTEP_OK) return rc;
+    const int32_t end = f0 + C;
+    const int32_t lo = f0 - W > 0 ? f0 - W : 0;
+    const int32_t n_sink = S_ < lo ? S_ : lo;
+    int32_t missing = first_missing(0, n_sink, newest);
+    if (missing == n_sink && (missing = first_missing(lo, end, newest)) == end) missing = -1;
+    if (missing >= 0) return fail(UNSTEP_E_STATE, "frame " + std::to_string(missing) + " is not in the cache", why);
     Segments s;
-    for (int32_t f : frames) {
-      const int32_t r0 = slot(f) * T_;
+    auto add = [&](int32_t slot0, int32_t frames) {
+      if (frames <= 0) return;
+      const int32_t r0 = slot0 * T_;
       if (s.n > 0 && s.row0[s.n - 1] + s.len[s.n - 1] == r0) {
-        s.len[s.n - 1] += T_;
+        s.len[s.n - 1] += frames * T_;
       } else {
-        if (s.n == UNSTEP_MAX_SEGMENTS) return fail(UNSTEP_E_RANGE, "too many key segments", why);
         s.row0[s.n] = r0;
-        s.len[s.n] = T_;
-        ++s.n;
+        s.len[s.n++] = frames * T_;
       }
+    };
+    add(0, n_sink);
+    add(lo, (S_ < end ? S_ : end) - lo);               // the window's own sinks
+    const int32_t ring = lo > S_ ? lo : S_;            // its ring frames, in two runs where the ring wraps
+    if (ring < end) {
+      const int32_t first = std::min(end - ring, R_ - (ring - S_) % R_);
+      add(slot(ring), first);
+      add(S_, end - ring - first);
     }
     *out = s;
     return UNSTEP_OK;

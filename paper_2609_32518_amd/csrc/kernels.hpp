@@ -39,6 +39,43 @@ constexpr int kNormMaxHeads = 32;
 
 hipError_t launch_rope_append(const RopeAppendArgs& a, hipStream_t stream);
 
+// The rotating append with its options: interleaved or half layout over the first `rot` dimensions of a
+// head, and either a bf16 cache or a quantised one.
+struct RotaryAppendArgs {
+  RopeAppendArgs a;        // cos_t, sin_t: [N, rot / 2]; q_rot, k_cache, v_cache: the bf16 outputs
+  int32_t half;            // 1: pairs (j, j + rot / 2), 0: pairs (2j, 2j + 1)
+  int32_t rot;             // a multiple of 16, at most 128
+  // quantised outputs (k8 non-null switches them on): e4m3 rows of 128 and four scale bytes each, in
+  // the places of q_rot, k_cache and v_cache
+  uint8_t *q8, *q_scale, *k8, *k_scale, *v8, *v_scale;
+  float q_mul;             // the quantised queries' factor
+};
+hipError_t launch_rotary_append(const RotaryAppendArgs& a, hipStream_t stream);
+
+// cos/sin tables of a chunk: pair j < pairs_t turns with the frame, the next pairs_h with the row, the
+// last pairs_w with the column, by freq[j] per position.
+struct RotaryTableArgs {
+  double freq[kHeadDim / 2];
+  double amplitude;
+  float *cos_t, *sin_t;    // [frames * grid_h * grid_w, pairs]
+  int32_t f0, frames, grid_h, grid_w;
+  int32_t pairs_t, pairs_h, pairs_w;
+};
+hipError_t launch_rotary_tables(const RotaryTableArgs& a, hipStream_t stream);
+
+// bf16 values of quantised rows of 128: output row i is row i of x8, or the row of a cache that holds
+// token (b, n, h) of the frames from f0 on.
+struct Mx8ReadArgs {
+  const uint8_t *x8, *x_scale;
+  uint16_t* out;
+  int64_t rows;            // rows of the output
+  // a cache read (T > 0): output row ((b N + n) H + h) is the row of token n of the frames from f0 on
+  int32_t B, H, T, C, slots, f0, S, R;
+  const uint8_t *y8, *y_scale;   // a second tensor of the same places into y_out, or null
+  uint16_t* y_out;
+};
+hipError_t launch_mx8_read(const Mx8ReadArgs& a, hipStream_t stream);
+
 // Attention tiling: 256 queries per work-group (8 waves x 32), 64 keys per tile, and at most
 // one work-group per compute unit (256 on MI355X) in the balanced schedule.
 constexpr int kAttnBlockQ = 256;
@@ -122,6 +159,18 @@ constexpr size_t kAttnMaxWorkspace = attn_workspace_bytes(kAttnMaxGroups);
 AttnPlan attn_plan(int32_t B, int32_t H, int32_t N, int32_t n_keys, size_t scratch = kAttnMaxWorkspace);
 
 hipError_t launch_window_attn(const AttnArgs& a, hipStream_t stream);
+// The merge of a split launch's partials (nothing for a launch without them).
+hipError_t launch_attn_combine(const AttnArgs& a, hipStream_t stream);
+
+// Attention of quantised queries over a quantised cache: `a` as above (its q, k_cache and v_cache are not
+// read), scores in base-2 units (a.scale is ln 2, so offsets and sums merge as those of bf16 launches).
+struct Mx8AttnArgs {
+  AttnArgs a;
+  const uint8_t *q8, *q_scale;   // [B, N, H, 128], [B, N, H, 4]
+  const uint8_t *k8, *k_scale;   // [B, H, slots, 128], [B, H, slots, 4]
+  const uint8_t *v8, *v_scale;
+};
+hipError_t launch_mx8_attn(const Mx8AttnArgs& a, hipStream_t stream);
 
 // The allocation-free entry point's scratch on the current device: a static device array of
 // kAttnMaxWorkspace bytes whose device address is looked up once per device and kept.

@@ -49,6 +49,7 @@
 #include <climits>
 #include <mutex>
 
+#include "attn_schedule.hpp"
 #include "kernels.hpp"
 #include "seg_table.hpp"
 
@@ -408,16 +409,6 @@ __device__ __forceinline__ void walk(Acc& a, Walk& w, const bf16x8_t (&qf)[8], i
   if (group == 0) barrier();                   // group A idles in the last phase
 }
 
-__device__ __forceinline__ Schedule make_schedule(const AttnArgs& a, int32_t* qtiles_out) {
-  const int32_t qtiles = (a.N + kBlockQ - 1) / kBlockQ;
-  *qtiles_out = qtiles;
-  Schedule sc;
-  sc.Tk = (a.n_keys + kBlockK - 1) / kBlockK;
-  sc.U = int64_t(a.B) * a.H * qtiles * sc.Tk;
-  sc.G = a.groups;
-  return sc;
-}
-
 // kParts: a whole number of work-groups per query tile (a.parts), so one segment each, found
 // without the 64-bit divisions of the general split.
 template <bool kParts>
@@ -758,7 +749,11 @@ hipError_t launch_window_attn(const AttnArgs& a, hipStream_t stream) {
   else
     hipLaunchKernelGGL(window_attn_kernel<false>, dim3(unsigned(a.groups)), dim3(kThreads), 0, stream, a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.part_o == nullptr) return e;
+  return e == hipSuccess ? launch_attn_combine(a, stream) : e;
+}
+
+hipError_t launch_attn_combine(const AttnArgs& a, hipStream_t stream) {
+  if (a.part_o == nullptr) return hipSuccess;
   switch (a.parts ? attn_merge_slices(a.B * a.H * ((a.N + kBlockQ - 1) / kBlockQ), a.parts) : 1) {
     case 1: launch_combine<1>(a, stream); break;
     case 2: launch_combine<2>(a, stream); break;
