@@ -38,12 +38,20 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) i16x4_t lds_i16x4_t;
+typedef __attribute__((address_space(3))) u32x4_t lds_u32x4_t;
+typedef __attribute__((address_space(3))) uint32_t lds_u32_t;
+typedef __attribute__((address_space(3))) bf16x4_t lds_bf16x4_t;
+typedef __attribute__((address_space(3))) void lds_void_t;
 
+// LDS slots of 16 bytes are XOR-swizzled by the row: 256-byte V rows so that the transposing reads (4 rows x
+// 4 slots per half-wave), 128-byte K rows so that the fragment reads (16 rows at one slot), meet no bank twice.
 __device__ __forceinline__ int swz16(int row) { return ((row & 3) << 2) | ((row >> 2) & 3); }
 __device__ __forceinline__ int swz8(int row) { return (row >> 1) & 7; }
 
-__device__ __forceinline__ u32x2_t lds_read_tr(const uint8_t* p) {
-  const i16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t*)(p));
+// Transposing LDS read: within each 16-lane group, lane i receives element (i & 3) of the 4 x b16 rows
+// addressed by lanes 4e + (i >> 2), e = 0..3.
+__device__ __forceinline__ u32x2_t lds_read_tr(uint32_t addr) {
+  const i16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t*)(uintptr_t)(addr));
   return __builtin_bit_cast(u32x2_t, v);
 }
 
@@ -62,145 +70,416 @@ __device__ __forceinline__ i32x8_t join(u32x4_t a, u32x4_t b) {
   return i32x8_t{int(a.x), int(a.y), int(a.z), int(a.w), int(b.x), int(b.y), int(b.z), int(b.w)};
 }
 
+// ---- the walk of a 256-query tile over a key range -------------------------------------------------
+//
+// Work-group: 8 waves of 32 queries.  Waves w and w + 4 share a SIMD and run half a tile apart (groups A
+// and B): in each phase one of them multiplies while the other computes the softmax of its tile.  Per
+// 64-key tile t:
+//   M phase: O^T += V^T(t-1) P^T(t-1) (16 bf16 products) and S^T(t) = K(t) Q^T - m (4 scaled 8-bit ones)
+//   V phase: this thread's 16 bytes of K(t+2) and of V(t+1), loaded a tile ago, go to LDS, V as bf16;
+//            those of K(t+3) and V(t+2) are loaded; P(t) = exp2(S(t)) in bf16, row sums
+// K tiles in LDS: ring of three, K(u) written in V phase u - 2, which for group B is the phase before group
+// A's M phase u, and overwriting K(u-3), last read one phase before group A's write.  V tiles: ring of
+// three, V(u) written in V phase u - 1 and read in M phase u + 1.  One barrier per phase.
+//
+// The exponent offset m is the row's maximum over the range's first tile and enters the product as its
+// accumulator, so a score costs one exp2, one add and half a conversion; a row whose sum passes 2^64
+// makes the work-group redo its range with the exact maximum.
+constexpr int kRing = 3;
+constexpr int kTile8 = kBlockK * kRow8, kTile16 = kBlockK * kRow16, kTileS = kBlockK * kMxBlocks;
+constexpr int kLdsV = kRing * kTile8, kLdsS = kLdsV + kRing * kTile16, kLdsBytes = kLdsS + kRing * kTileS;
+// output staging of a finished query tile in the rings: 272-byte rows
+constexpr int kOutPitch = kRow16 + 16;
+static_assert(kBlockQ * kOutPitch <= kLdsBytes, "the output tile must fit the rings");
+constexpr int kFetchAhead = 4;               // fragments read ahead of the product that uses them
+
+struct Walk {
+  const uint8_t *k8, *v8, *ks, *vs;          // this (batch, head)'s rows
+  SegTable seg;
+  int32_t k_begin, k_end, n;                 // logical key range, its tiles
+  int half;
+  int lrow;                                  // loader: tile row of this thread
+  uint32_t lpiece, lscale;                   // ... byte in the row, scale byte of the row
+  RowCursor kc, vc;                          // ... cursors of ranges of several runs
+  uint32_t wk, wv[2], ws;                    // LDS addresses of what it writes, in slot 0
+  uint32_t koff[4], soff;                    // LDS: K fragment halves of d-steps 0, 1; scale words
+  uint32_t voff[2][4];                       // LDS: V^T fragment (upper 8 keys, d block)
+};
+
+struct Stage {
+  u32x4_t k, v;
+  uint32_t ks, vs;
+};
+
+struct Acc {
+  f32x16_t o[4];               // O^T: head dims 32 d .. 32 d + 31 x the wave's 32 queries
+  f32x16_t s[2];               // S^T of the current tile: keys 32 kb .. 32 kb + 31
+  bf16x8_t p[2][2];            // P^T of the previous tile: (key block, 16-key step)
+  f32x16_t negm;               // - exponent offset, in every element
+  float l;                     // row sum (this lane's half of the keys)
+  float mx;                    // running row max (max-only walk)
+};
+
+__device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+template <bool kOneRun>
+__device__ __forceinline__ int32_t stage_row(const Walk& w, RowCursor& c, int32_t kt0) {
+  int32_t row[1];
+  tile_rows<kOneRun, kBlockK, 1, 1>(w.seg, w.k_end, c, kt0, w.lrow, row);
+  return row[0];
+}
+
+// This thread's 16 bytes of a K tile (its row's scale word with them), and of a V tile (their block's byte).
+template <bool kOneRun>
+__device__ __forceinline__ void load_k(Stage& st, Walk& w, int32_t t) {
+  const uint32_t row = uint32_t(stage_row<kOneRun>(w, w.kc, w.k_begin + t * kBlockK));
+  st.k = *reinterpret_cast<const u32x4_t*>(w.k8 + (row * uint32_t(kRow8) + w.lpiece));
+  st.ks = *reinterpret_cast<const uint32_t*>(w.ks + row * uint32_t(kMxBlocks));
+}
+template <bool kOneRun>
+__device__ __forceinline__ void load_v(Stage& st, Walk& w, int32_t t) {
+  const uint32_t row = uint32_t(stage_row<kOneRun>(w, w.vc, w.k_begin + t * kBlockK));
+  st.v = *reinterpret_cast<const u32x4_t*>(w.v8 + (row * uint32_t(kRow8) + w.lpiece));
+  st.vs = w.vs[row * uint32_t(kMxBlocks) + w.lscale];
+}
+__device__ __forceinline__ void store_k(const Stage& st, const Walk& w, int slot) {
+  *reinterpret_cast<lds_u32x4_t*>(uintptr_t(w.wk + slot * kTile8)) = st.k;
+  if (w.lpiece == 0) *reinterpret_cast<lds_u32_t*>(uintptr_t(w.ws + slot * kTileS)) = st.ks;
+}
+__device__ __forceinline__ void store_v(const Stage& st, const Walk& w, int slot) {
+  u32x4_t b[2];
+  to_bf16(st.v, mx8_scale(st.vs), b);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) *reinterpret_cast<lds_u32x4_t*>(uintptr_t(w.wv[i] + slot * kTile16)) = b[i];
+}
+
+struct Queries {
+  i32x8_t f[2];                // d-steps of 64
+  int scale;
+};
+
+// Jobs of an M phase: 0..15 the PV product (key block j / 8, 16-key step (j / 4) % 2, d block j % 4),
+// 16..19 the QK product (key block (j - 16) / 2, d-step (j - 16) % 2).  Issue order: a QK job after every
+// four PV jobs, so that the two steps into one accumulator are apart.
+__device__ __forceinline__ constexpr int job_id(int i) { return i % 5 == 4 ? 16 + i / 5 : i - i / 5; }
+
+union Frag {
+  u32x4_t r[2];
+};
+
+__device__ __forceinline__ Frag fetch(int j, int kslot, int vslot, const Walk& w) {
+  Frag f;
+  if (j < 16) {
+    const uint32_t rel = vslot * kTile16 + (32 * (j >> 3) + 16 * ((j >> 2) & 1)) * kRow16;
+    const u32x2_t lo = lds_read_tr(w.voff[0][j & 3] + rel), hi = lds_read_tr(w.voff[1][j & 3] + rel);
+    f.r[0] = u32x4_t{lo.x, lo.y, hi.x, hi.y};
+  } else {
+    const uint32_t rel = kslot * kTile8 + 32 * ((j - 16) >> 1) * kRow8;
+    const int st = j & 1;
+    f.r[0] = *reinterpret_cast<const lds_u32x4_t*>(uintptr_t(w.koff[2 * st] + rel));
+    f.r[1] = *reinterpret_cast<const lds_u32x4_t*>(uintptr_t(w.koff[2 * st + 1] + rel));
+  }
+  return f;
+}
+
+template <bool kZero>
+__device__ __forceinline__ void run(Acc& a, int j, const Frag& f, const uint32_t (&ks)[2], const Queries& q) {
+  if (j < 16) {
+    a.o[j & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, f.r[0]), a.p[j >> 3][(j >> 2) & 1],
+                                                         a.o[j & 3], 0, 0, 0);
+  } else {
+    const int kb = (j - 16) >> 1;
+    const f32x16_t zero = {};
+    if (j & 1)
+      a.s[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(join(f.r[0], f.r[1]), q.f[1], a.s[kb], 0, 0, 2, int(ks[kb]), 2, q.scale);
+    else
+      a.s[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(join(f.r[0], f.r[1]), q.f[0], kZero ? zero : a.negm, 0, 0, 0,
+                                                                int(ks[kb]), 0, q.scale);
+  }
+}
+
+// kPart 0: all 20 jobs; 1: the QK jobs alone (a walk's first tile); 2: the PV jobs alone (after its last).
+template <int kPart>
+__device__ __forceinline__ constexpr int jobs() { return kPart == 0 ? 20 : kPart == 1 ? 4 : 16; }
+template <int kPart>
+__device__ __forceinline__ constexpr int job_at(int i) { return kPart == 0 ? job_id(i) : kPart == 1 ? 16 + i : i; }
+
+template <int kPart, bool kZero, int J>
+struct MJob {
+  static __device__ __forceinline__ void go(Acc& a, Frag (&f)[jobs<kPart>()], int kslot, int vslot, const uint32_t (&ks)[2],
+                                            const Queries& q, const Walk& w) {
+    constexpr int kNext = J + kFetchAhead;
+    if constexpr (kNext < jobs<kPart>()) f[kNext] = fetch(job_at<kPart>(kNext), kslot, vslot, w);
+    run<kZero>(a, job_at<kPart>(J), f[J], ks, q);
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if constexpr (kNext < jobs<kPart>()) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    if constexpr (J + 1 < jobs<kPart>()) MJob<kPart, kZero, J + 1>::go(a, f, kslot, vslot, ks, q, w);
+  }
+};
+
+template <int kPart, bool kZero>
+__device__ __forceinline__ void m_phase(Acc& a, int kslot, int vslot, const Queries& q, const Walk& w) {
+  Frag f[jobs<kPart>()];
+  uint32_t ks[2] = {0, 0};
+  if (kPart != 2) {
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+      ks[kb] = *reinterpret_cast<const lds_u32_t*>(uintptr_t(w.soff + kslot * kTileS + 32 * kb * kMxBlocks)) >> (8 * w.half);
+  }
+#pragma unroll
+  for (int i = 0; i < kFetchAhead; ++i) f[i] = fetch(job_at<kPart>(i), kslot, vslot, w);
+  __builtin_amdgcn_sched_group_barrier(0x100, 2 * kFetchAhead + (kPart != 2 ? 2 : 0), 0);
+  MJob<kPart, kZero, 0>::go(a, f, kslot, vslot, ks, q, w);
+}
+
+// The loader's part of V phase t (kSlot = t % 3): what it loaded a tile ago goes to LDS, the next loads start.
+template <int kSlot, bool kOneRun>
+__device__ __forceinline__ void turn_stage(Stage& st, Walk& w, int32_t t) {
+  if (t + 2 < w.n) store_k(st, w, (kSlot + 2) % kRing);
+  if (t + 1 < w.n) store_v(st, w, (kSlot + 1) % kRing);
+  if (t + 3 < w.n) load_k<kOneRun>(st, w, t + 3);
+  if (t + 2 < w.n) load_v<kOneRun>(st, w, t + 2);
+}
+
+// kMode 0: offsets from the first tile; 1: offsets given; 2: row max only.
+template <int kMode, bool kFirst>
+__device__ __forceinline__ void softmax(Acc& a, int32_t t, const Walk& w) {
+  const int32_t kt0 = w.k_begin + t * kBlockK;
+  if (kt0 + kBlockK > w.k_end) {
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (kt0 + 32 * kb + 8 * (i >> 2) + 4 * w.half + (i & 3) >= w.k_end) a.s[kb][i] = -INFINITY;
+  }
+  if (kMode == 2) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) a.mx = fmaxf(a.mx, fmaxf(a.s[0][i], a.s[1][i]));
+    return;
+  }
+  if (kMode == 0 && kFirst) {
+    float m = a.s[0][0];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) m = fmaxf(fmaxf(m, a.s[0][i]), a.s[1][i]);
+    m = fmaxf(m, __shfl_xor(m, 32));
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      a.negm[i] = -m;
+      a.s[0][i] -= m;
+      a.s[1][i] -= m;
+    }
+  }
+  float acc0 = 0.f, acc1 = 0.f;
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const float e0 = __builtin_amdgcn_exp2f(a.s[kb][i]);
+      const float e1 = __builtin_amdgcn_exp2f(a.s[kb][i + 1]);
+      acc0 += e0;
+      acc1 += e1;
+      a.p[kb][i >> 3][i & 7] = (__bf16)e0;
+      a.p[kb][i >> 3][(i & 7) + 1] = (__bf16)e1;
+    }
+  a.l += acc0 + acc1;
+}
+
+template <int kMode, int kSlot, bool kOneRun, bool kIdle, bool kFirst = false>
+__device__ __forceinline__ void step(Acc& a, Stage& st, Walk& w, const Queries& q, int32_t t) {
+  if (t >= w.n) return;
+  if (!kIdle) m_phase<kFirst ? 1 : 0, (kFirst && kMode == 0) || kMode == 2>(a, kSlot, (kSlot + 2) % kRing, q, w);
+  barrier();
+  turn_stage<kSlot, kOneRun>(st, w, t);
+  if (!kIdle) softmax<kMode, kFirst>(a, t, w);
+  barrier();
+}
+
+// Frees the rings and fills their first slots (K 0, K 1, V 0); K 2 and V 1 are on their way.
+template <bool kOneRun>
+__device__ __forceinline__ void walk_begin(Stage& st, Walk& w) {
+  if (!kOneRun) {
+    cursor_at(w.seg, w.k_end, w.k_begin, w.kc);
+    w.vc = w.kc;
+  }
+  Stage second;
+  load_k<kOneRun>(st, w, 0);
+  load_v<kOneRun>(st, w, 0);
+  if (w.n > 1) load_k<kOneRun>(second, w, 1);
+  __syncthreads();
+  store_k(st, w, 0);
+  store_v(st, w, 0);
+  if (w.n > 1) store_k(second, w, 1);
+  if (w.n > 2) load_k<kOneRun>(st, w, 2);
+  if (w.n > 1) load_v<kOneRun>(st, w, 1);
+}
+
+template <int kMode, bool kOneRun, bool kIdle>
+__device__ __forceinline__ void walk(Acc& a, Stage& st, Walk& w, const Queries& q, int group) {
+  const f32x16_t zero = {};
+#pragma unroll
+  for (int d = 0; d < 4; ++d) a.o[d] = zero;
+  a.l = 0.f;
+  a.mx = -INFINITY;
+  barrier();                                   // the first slots are complete: global phase 0
+  if (group == 1) barrier();                   // group B idles in phase 0
+  step<kMode, 0, kOneRun, kIdle, true>(a, st, w, q, 0);
+  for (int32_t t0 = 1; t0 < w.n; t0 += kRing) {
+    step<kMode, 1, kOneRun, kIdle>(a, st, w, q, t0);
+    step<kMode, 2, kOneRun, kIdle>(a, st, w, q, t0 + 1);
+    step<kMode, 0, kOneRun, kIdle>(a, st, w, q, t0 + 2);
+  }
+  if (!kIdle && kMode != 2) m_phase<2, false>(a, 0, (w.n - 1) % kRing, q, w);
+  barrier();
+  if (group == 0) barrier();                   // group A idles in the last phase
+}
+
+// A whole range: offsets from its first tile, and again with the exact maxima where a sum left its range
+// (rare, so it has one path, with the loader of any number of runs).
+template <bool kIdle>
+__device__ __forceinline__ void walk_again(Acc& a, Stage& st, Walk& w, const Queries& q, int group) {
+  walk_begin<false>(st, w);
+  walk<2, false, kIdle>(a, st, w, q, group);
+  const float m = fmaxf(a.mx, __shfl_xor(a.mx, 32));
+#pragma unroll
+  for (int i = 0; i < 16; ++i) a.negm[i] = -m;
+  walk_begin<false>(st, w);
+  walk<1, false, kIdle>(a, st, w, q, group);
+}
+
+// kParts: a whole number of work-groups per query tile (a.parts), one segment each.
+template <bool kParts>
 __global__ __launch_bounds__(kThreads) void mx8_attn_kernel(Mx8AttnArgs m) {
-  __shared__ __attribute__((aligned(1024))) uint8_t kt[kBlockK * kRow8];
-  __shared__ __attribute__((aligned(1024))) uint8_t vt[kBlockK * kRow16];
-  __shared__ uint32_t ks[kBlockK];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kLdsBytes];
   const AttnArgs& a = m.a;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, col = lane & 31;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int group = wave >> 2, half = lane >> 5, col = lane & 31;
   const int32_t N = a.N, H = a.H, G = gridDim.x;
+  // hardware work-group i runs on XCD i % 8: each XCD gets a contiguous range of logical work-groups
   const int32_t xcd = blockIdx.x % kXcds;
   const int32_t g = xcd * (G / kXcds) + min(xcd, G % kXcds) + blockIdx.x / kXcds;
   int32_t qtiles;
   const Schedule sc = make_schedule(a, &qtiles);
-  SegTable seg{a.seg_l0[1], a.seg_l0[2], a.seg_l0[3], a.seg_row0[0], a.seg_row0[1], a.seg_row0[2], a.seg_row0[3]};
 
-  const int64_t u_begin = sc.start(g);
-  int64_t u_hi = sc.start(int64_t(g) + 1);
+  Walk w;
+  w.seg = SegTable{a.seg_l0[1], a.seg_l0[2], a.seg_l0[3], a.seg_row0[0], a.seg_row0[1], a.seg_row0[2], a.seg_row0[3]};
+  w.half = half;
+  const uint32_t lds0 = uint32_t(uintptr_t((lds_void_t*)lds));
+  w.lrow = tid >> 3;
+  {
+    const int ts = tid & 7;
+    w.lpiece = 16 * ts;
+    w.lscale = ts >> 1;
+    w.wk = lds0 + w.lrow * kRow8 + (ts ^ swz8(w.lrow)) * 16;
+    w.ws = lds0 + kLdsS + w.lrow * kMxBlocks;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) w.wv[i] = lds0 + kLdsV + w.lrow * kRow16 + ((2 * ts + i) ^ swz16(w.lrow)) * 16;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w.koff[i] = lds0 + col * kRow8 + ((2 * i + half) ^ swz8(col)) * 16;
+  w.soff = lds0 + kLdsS + col * kMxBlocks;
+  {
+    const int e = (lane & 15) >> 2, q = lane & 3, g16 = lane >> 4;
+#pragma unroll
+    for (int up = 0; up < 2; ++up)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        const int row = 8 * up + 4 * half + e;
+        const int piece = 4 * d + 2 * (g16 & 1) + (q >> 1);
+        w.voff[up][d] = lds0 + kLdsV + row * kRow16 + (piece ^ swz16(row)) * 16 + (q & 1) * 8;
+      }
+  }
+
+  const int64_t u_begin = kParts ? 0 : sc.start(g);
+  int64_t u_hi = kParts ? 0 : sc.start(int64_t(g) + 1);
   do {
-    const Segment sg = take_segment(sc, u_begin, u_hi);
+    const Segment sg = kParts ? part_segment(sc.Tk, a.parts, g) : take_segment(sc, u_begin, u_hi);
     const int32_t t = int32_t(sg.t), qt = t % qtiles, bh = t / qtiles, h = bh % H, b = bh / H;
     const int64_t row0 = int64_t(bh) * a.slots;
-    const int32_t k_begin = sg.k0 * kBlockK, k_end = min(a.n_keys, sg.k1 * kBlockK);
+    w.k8 = m.k8 + row0 * kRow8;
+    w.v8 = m.v8 + row0 * kRow8;
+    w.ks = m.k_scale + row0 * kMxBlocks;
+    w.vs = m.v_scale + row0 * kMxBlocks;
+    w.k_begin = sg.k0 * kBlockK;
+    w.k_end = min(a.n_keys, sg.k1 * kBlockK);
+    w.n = (w.k_end - w.k_begin + kBlockK - 1) / kBlockK;
+    const bool one_run = w.k_end <= w.seg.l1;
+    Stage st;
+    if (one_run)
+      walk_begin<true>(st, w);
+    else
+      walk_begin<false>(st, w);
+
     const int32_t r = wave * 32 + col, qi = qt * kBlockQ + r;
-    i32x8_t qf[2];
-    uint32_t qs;
+    Queries q;
     {
       const int64_t qrow = (int64_t(b) * N + min(qi, N - 1)) * H + h;
       const u32x4_t* qp = reinterpret_cast<const u32x4_t*>(m.q8 + qrow * kRow8 + 16 * half);
-      qf[0] = join(qp[0], qp[2]);
-      qf[1] = join(qp[4], qp[6]);
-      qs = *reinterpret_cast<const uint32_t*>(m.q_scale + qrow * kMxBlocks) >> (8 * half);
+      q.f[0] = join(qp[0], qp[2]);
+      q.f[1] = join(qp[4], qp[6]);
+      q.scale = int(*reinterpret_cast<const uint32_t*>(m.q_scale + qrow * kMxBlocks) >> (8 * half));
     }
-    f32x16_t o[4] = {};
-    float l = 0.f, mx = -INFINITY;
-    for (int32_t k0 = k_begin; k0 < k_end; k0 += kBlockK) {
-      __syncthreads();
-      {
-        const int tr = tid >> 3, ts = tid & 7;
-        const int64_t row = row0 + seg.row(min(k0 + tr, k_end - 1));
-        const u32x4_t kx = *reinterpret_cast<const u32x4_t*>(m.k8 + row * kRow8 + 16 * ts);
-        const u32x4_t vx = *reinterpret_cast<const u32x4_t*>(m.v8 + row * kRow8 + 16 * ts);
-        u32x4_t vb[2];
-        to_bf16(vx, mx8_scale(m.v_scale[row * kMxBlocks + (ts >> 1)]), vb);
-        *reinterpret_cast<u32x4_t*>(kt + tr * kRow8 + ((ts ^ swz8(tr)) * 16)) = kx;
+    Acc acc;
+    // a wave whose 32 queries all lie past the chunk's end runs the loads and barriers only
+    const bool idle = qt * kBlockQ + wave * 32 >= N;
+    if (one_run)
+      idle ? walk<0, true, true>(acc, st, w, q, group) : walk<0, true, false>(acc, st, w, q, group);
+    else
+      idle ? walk<0, false, true>(acc, st, w, q, group) : walk<0, false, false>(acc, st, w, q, group);
+    if (__syncthreads_or(!idle && !(acc.l <= 0x1p64f)))
+      idle ? walk_again<true>(acc, st, w, q, group) : walk_again<false>(acc, st, w, q, group);
+
+    const float l_tot = acc.l + __shfl_xor(acc.l, 32), off = -acc.negm[0];
+    if (sg.full) {
+      // the tile's rows go out through the rings as whole 256-byte rows; rows past the end are staged, not stored
+      barrier();
+      const float inv = 1.f / l_tot;
+      const uint32_t orow = lds0 + uint32_t(r * kOutPitch + 8 * half);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-          *reinterpret_cast<u32x4_t*>(vt + tr * kRow16 + (((2 * ts + i) ^ swz16(tr)) * 16)) = vb[i];
-        if (ts == 0) ks[tr] = *reinterpret_cast<const uint32_t*>(m.k_scale + row * kMxBlocks);
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int gg = 0; gg < 4; ++gg) {
+          bf16x4_t rr;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) rr[e] = (__bf16)(acc.o[d][4 * gg + e] * inv);
+          *reinterpret_cast<lds_bf16x4_t*>(uintptr_t(orow + (d * 32 + 8 * gg) * 2)) = rr;
+        }
+      barrier();
+      const int pc = tid & 15;
+#pragma unroll
+      for (int i = 0; i < kBlockQ / (kThreads / 16); ++i) {
+        const int rs = (tid >> 4) + (kThreads / 16) * i;
+        const int32_t qs = qt * kBlockQ + rs;
+        const u32x4_t v = *reinterpret_cast<const lds_u32x4_t*>(uintptr_t(lds0 + uint32_t(rs * kOutPitch + pc * 16)));
+        if (qs < N) *reinterpret_cast<u32x4_t*>(a.out + ((int64_t(b) * N + qs) * H + h) * kHeadDim + 8 * pc) = v;
       }
-      __syncthreads();
-      f32x16_t s[2] = {};
+      if (qi < N && a.lse && half == 0) a.lse[(int64_t(b) * H + h) * N + qi] = off * a.scale + logf(l_tot);
+    } else if (qi < N) {
+      const int64_t prow = (int64_t(g) * 2 + sg.slot) * kBlockQ + r;
+      const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+      float* op = a.part_o + prow * kHeadDim + 4 * half;
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        const int row = 32 * kb + col;
-        const uint32_t sc8 = ks[row] >> (8 * half);
-        const u32x4_t* base = reinterpret_cast<const u32x4_t*>(kt + row * kRow8);
-        const int x = swz8(row);
-        const i32x8_t f0 = join(base[half ^ x], base[(2 + half) ^ x]);
-        const i32x8_t f1 = join(base[(4 + half) ^ x], base[(6 + half) ^ x]);
-        s[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f0, qf[0], s[kb], 0, 0, 0, int(sc8), 0, int(qs));
-        s[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f1, qf[1], s[kb], 0, 0, 2, int(sc8), 2, int(qs));
-      }
-      float top = mx;
+      for (int d = 0; d < 4; ++d)
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          if (k0 + 32 * kb + 8 * (i >> 2) + 4 * half + (i & 3) >= k_end) s[kb][i] = -INFINITY;
-          top = fmaxf(top, s[kb][i]);
-        }
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float shrink = __builtin_amdgcn_exp2f(mx - top);
-      mx = top;
-      l *= shrink;
-      bf16x8_t p[2][2];
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float e = __builtin_amdgcn_exp2f(s[kb][i] - top);
-          l += e;
-          p[kb][i >> 3][i & 7] = (__bf16)e;
-        }
-#pragma unroll
-      for (int d = 0; d < 4; ++d) o[d] *= shrink;
-      const int e = (lane & 15) >> 2, q = lane & 3, g16 = lane >> 4;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int st = 0; st < 2; ++st)
-#pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            u32x2_t f[2];
-#pragma unroll
-            for (int up = 0; up < 2; ++up) {
-              const int row = 32 * kb + 16 * st + 8 * up + 4 * half + e;
-              const int piece = 4 * d + 2 * (g16 & 1) + (q >> 1);
-              f[up] = lds_read_tr(vt + row * kRow16 + (piece ^ swz16(row)) * 16 + (q & 1) * 8);
-            }
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                __builtin_bit_cast(bf16x8_t, u32x4_t{f[0].x, f[0].y, f[1].x, f[1].y}), p[kb][st], o[d], 0, 0, 0);
-          }
-    }
-    const float l_tot = l + __shfl_xor(l, 32);
-    if (qi < N) {
-      if (sg.full) {
-        const float inv = 1.f / l_tot;
-        uint16_t* op = a.out + ((int64_t(b) * N + qi) * H + h) * kHeadDim + 4 * half;
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-          for (int gg = 0; gg < 4; ++gg) {
-            bf16x4_t rr;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) rr[e] = (__bf16)(o[d][4 * gg + e] * inv);
-            *reinterpret_cast<bf16x4_t*>(op + d * 32 + 8 * gg) = rr;
-          }
-        if (a.lse && half == 0) a.lse[(int64_t(b) * H + h) * N + qi] = mx * a.scale + logf(l_tot);
-      } else {
-        const int64_t prow = (int64_t(g) * 2 + sg.slot) * kBlockQ + r;
-        const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
-        float* op = a.part_o + prow * kHeadDim + 4 * half;
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-          for (int gg = 0; gg < 4; ++gg)
-            *reinterpret_cast<float4*>(op + d * 32 + 8 * gg) =
-                make_float4(o[d][4 * gg] * inv, o[d][4 * gg + 1] * inv, o[d][4 * gg + 2] * inv, o[d][4 * gg + 3] * inv);
-        if (half == 0) {
-          a.part_ml[prow * 2] = l_tot > 0.f ? mx : -INFINITY;
-          a.part_ml[prow * 2 + 1] = l_tot;
-        }
+        for (int gg = 0; gg < 4; ++gg)
+          *reinterpret_cast<float4*>(op + d * 32 + 8 * gg) =
+              make_float4(acc.o[d][4 * gg] * inv, acc.o[d][4 * gg + 1] * inv, acc.o[d][4 * gg + 2] * inv,
+                          acc.o[d][4 * gg + 3] * inv);
+      if (half == 0) {
+        a.part_ml[prow * 2] = l_tot > 0.f ? off : -INFINITY;
+        a.part_ml[prow * 2 + 1] = l_tot;
       }
     }
-  } while (u_hi > u_begin);
+  } while (!kParts && u_hi > u_begin);
 }
 
 }  // namespace
 
 hipError_t launch_mx8_attn(const Mx8AttnArgs& m, hipStream_t stream) {
-  hipLaunchKernelGGL(mx8_attn_kernel, dim3(unsigned(m.a.groups)), dim3(kThreads), 0, stream, m);
+  if (m.a.parts)
+    hipLaunchKernelGGL(mx8_attn_kernel<true>, dim3(unsigned(m.a.groups)), dim3(kThreads), 0, stream, m);
+  else
+    hipLaunchKernelGGL(mx8_attn_kernel<false>, dim3(unsigned(m.a.groups)), dim3(kThreads), 0, stream, m);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? launch_attn_combine(m.a, stream) : e;
 }
