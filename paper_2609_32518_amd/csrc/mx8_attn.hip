@@ -230,6 +230,10 @@ __device__ __forceinline__ void m_phase(Acc& a, int kslot, int vslot, const Quer
   for (int i = 0; i < kFetchAhead; ++i) f[i] = fetch(job_at<kPart>(i), kslot, vslot, w);
   __builtin_amdgcn_sched_group_barrier(0x100, 2 * kFetchAhead + (kPart != 2 ? 2 : 0), 0);
   MJob<kPart, kZero, 0>::go(a, f, kslot, vslot, ks, q, w);
+  // the products stay in this phase: their results are first used after the barrier, past which the compiler
+  // would otherwise move them, into the other wave's multiplying phase
+  if (kPart != 2) asm volatile("" : "+v"(a.s[0]), "+v"(a.s[1]));
+  if (kPart != 1) asm volatile("" : "+v"(a.o[0]), "+v"(a.o[1]), "+v"(a.o[2]), "+v"(a.o[3]));
 }
 
 // The loader's part of V phase t (kSlot = t % 3): what it loaded a tile ago goes to LDS, the next loads start.
