@@ -87,28 +87,34 @@ __device__ __forceinline__ i32x8_t join(u32x4_t a, u32x4_t b) {
 // makes the work-group redo its range with the exact maximum.
 constexpr int kRing = 3;
 constexpr int kTile8 = kBlockK * kRow8, kTile16 = kBlockK * kRow16, kTileS = kBlockK * kMxBlocks;
-constexpr int kLdsV = kRing * kTile8, kLdsS = kLdsV + kRing * kTile16, kLdsBytes = kLdsS + kRing * kTileS;
+constexpr int kLdsV = kRing * kTile8, kLdsS = kLdsV + kRing * kTile16,
+              kLdsDump = kLdsS + kRing * kTileS, kLdsBytes = kLdsDump + kRing * kTileS;
 // output staging of a finished query tile in the rings: 272-byte rows
 constexpr int kOutPitch = kRow16 + 16;
 static_assert(kBlockQ * kOutPitch <= kLdsBytes, "the output tile must fit the rings");
 constexpr int kFetchAhead = 4;               // fragments read ahead of the product that uses them
 
 struct Walk {
-  const uint8_t *k8, *v8, *ks, *vs;          // this (batch, head)'s rows
+  const uint8_t *k8, *v8;                    // this (batch, head)'s rows
   SegTable seg;
   int32_t k_begin, k_end, n;                 // logical key range, its tiles
   int half;
   int lrow;                                  // loader: tile row of this thread
-  uint32_t lpiece, lscale;                   // ... byte in the row, scale byte of the row
+  uint32_t lpiece;                           // ... byte in the row
+  uint32_t lshift;                           // ... shift of its block's byte in the row's scale word
+  bool lkey;                                 // ... whether it loads the row's K scale word (else V's)
+  const uint8_t* lbase;                      // ... and those words
   RowCursor kc, vc;                          // ... cursors of ranges of several runs
   uint32_t wk, wv[2], ws;                    // LDS addresses of what it writes, in slot 0
   uint32_t koff[4], soff;                    // LDS: K fragment halves of d-steps 0, 1; scale words
   uint32_t voff[2][4];                       // LDS: V^T fragment (upper 8 keys, d block)
 };
 
+// What a thread has loaded of a K tile and of a V tile, and a scale word: the first of the 8 threads of a row
+// holds its K row's, the others their V row's.
 struct Stage {
   u32x4_t k, v;
-  uint32_t ks, vs;
+  uint32_t sc;
 };
 
 struct Acc {
@@ -129,26 +135,24 @@ __device__ __forceinline__ int32_t stage_row(const Walk& w, RowCursor& c, int32_
   return row[0];
 }
 
-// This thread's 16 bytes of a K tile (its row's scale word with them), and of a V tile (their block's byte).
+// The loads of K tile tk and V tile tv.
 template <bool kOneRun>
-__device__ __forceinline__ void load_k(Stage& st, Walk& w, int32_t t) {
-  const uint32_t row = uint32_t(stage_row<kOneRun>(w, w.kc, w.k_begin + t * kBlockK));
-  st.k = *reinterpret_cast<const u32x4_t*>(w.k8 + (row * uint32_t(kRow8) + w.lpiece));
-  st.ks = *reinterpret_cast<const uint32_t*>(w.ks + row * uint32_t(kMxBlocks));
-}
-template <bool kOneRun>
-__device__ __forceinline__ void load_v(Stage& st, Walk& w, int32_t t) {
-  const uint32_t row = uint32_t(stage_row<kOneRun>(w, w.vc, w.k_begin + t * kBlockK));
-  st.v = *reinterpret_cast<const u32x4_t*>(w.v8 + (row * uint32_t(kRow8) + w.lpiece));
-  st.vs = w.vs[row * uint32_t(kMxBlocks) + w.lscale];
+__device__ __forceinline__ void load_stage(Stage& st, Walk& w, int32_t tk, int32_t tv) {
+  const uint32_t rk = uint32_t(stage_row<kOneRun>(w, w.kc, w.k_begin + tk * kBlockK));
+  const uint32_t rv = uint32_t(stage_row<kOneRun>(w, w.vc, w.k_begin + tv * kBlockK));
+  st.k = *reinterpret_cast<const u32x4_t*>(w.k8 + (rk * uint32_t(kRow8) + w.lpiece));
+  st.v = *reinterpret_cast<const u32x4_t*>(w.v8 + (rv * uint32_t(kRow8) + w.lpiece));
+  st.sc = *reinterpret_cast<const uint32_t*>(w.lbase + (w.lkey ? rk : rv) * uint32_t(kMxBlocks));
 }
 __device__ __forceinline__ void store_k(const Stage& st, const Walk& w, int slot) {
   *reinterpret_cast<lds_u32x4_t*>(uintptr_t(w.wk + slot * kTile8)) = st.k;
-  if (w.lpiece == 0) *reinterpret_cast<lds_u32_t*>(uintptr_t(w.ws + slot * kTileS)) = st.ks;
+  *reinterpret_cast<lds_u32_t*>(uintptr_t(w.ws + slot * kTileS)) = st.sc;
 }
 __device__ __forceinline__ void store_v(const Stage& st, const Walk& w, int slot) {
+  // the first thread of a row takes the V word of the second
+  const uint32_t sc = uint32_t(__builtin_amdgcn_update_dpp(0, int(st.sc), 0xe5, 0xf, 0xf, false));   // quad_perm 1,1,2,3
   u32x4_t b[2];
-  to_bf16(st.v, mx8_scale(st.vs), b);
+  to_bf16(st.v, mx8_scale((sc >> w.lshift) & 0xffu), b);
 #pragma unroll
   for (int i = 0; i < 2; ++i) *reinterpret_cast<lds_u32x4_t*>(uintptr_t(w.wv[i] + slot * kTile16)) = b[i];
 }
@@ -236,18 +240,19 @@ __device__ __forceinline__ void m_phase(Acc& a, int kslot, int vslot, const Quer
   if (kPart != 1) asm volatile("" : "+v"(a.o[0]), "+v"(a.o[1]), "+v"(a.o[2]), "+v"(a.o[3]));
 }
 
-// The loader's part of V phase t (kSlot = t % 3): what it loaded a tile ago goes to LDS, the next loads start.
-template <int kSlot, bool kOneRun>
-__device__ __forceinline__ void turn_stage(Stage& st, Walk& w, int32_t t) {
-  if (t + 2 < w.n) store_k(st, w, (kSlot + 2) % kRing);
-  if (t + 1 < w.n) store_v(st, w, (kSlot + 1) % kRing);
-  if (t + 3 < w.n) load_k<kOneRun>(st, w, t + 3);
-  if (t + 2 < w.n) load_v<kOneRun>(st, w, t + 2);
-}
-
-// kMode 0: offsets from the first tile; 1: offsets given; 2: row max only.
-template <int kMode, bool kFirst>
-__device__ __forceinline__ void softmax(Acc& a, int32_t t, const Walk& w) {
+// V phase of tile t (kSlot = t % 3).  kMode 0: offsets from the first tile; 1: offsets given; 2: row max only.
+// The loader's part, in order: what was loaded a tile ago goes to LDS (K(t + 2) into the slot of K(t - 1),
+// V(t + 1) into that of V(t - 2)), K(t + 3) and V(t + 2) start; past the range's end it repeats the last
+// tile, whose copies nothing reads.  It runs between quarters of the softmax, so that the four waves of a phase do
+// not queue at the memory pipelines at once.
+template <int kMode, int kSlot, bool kOneRun, bool kIdle, bool kFirst>
+__device__ __forceinline__ void v_phase(Acc& a, Stage& st, Walk& w, int32_t t) {
+  if (kIdle) {
+    store_k(st, w, (kSlot + 2) % kRing);
+    store_v(st, w, (kSlot + 1) % kRing);
+    load_stage<kOneRun>(st, w, min(t + 3, w.n - 1), min(t + 2, w.n - 1));
+    return;
+  }
   const int32_t kt0 = w.k_begin + t * kBlockK;
   if (kt0 + kBlockK > w.k_end) {
 #pragma unroll
@@ -259,7 +264,6 @@ __device__ __forceinline__ void softmax(Acc& a, int32_t t, const Walk& w) {
   if (kMode == 2) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) a.mx = fmaxf(a.mx, fmaxf(a.s[0][i], a.s[1][i]));
-    return;
   }
   if (kMode == 0 && kFirst) {
     float m = a.s[0][0];
@@ -275,16 +279,24 @@ __device__ __forceinline__ void softmax(Acc& a, int32_t t, const Walk& w) {
   }
   float acc0 = 0.f, acc1 = 0.f;
 #pragma unroll
-  for (int kb = 0; kb < 2; ++kb)
+  for (int q = 0; q < 4; ++q) {
+    if (q == 0) store_k(st, w, (kSlot + 2) % kRing);
+    if (q == 1) store_v(st, w, (kSlot + 1) % kRing);
+    if (q == 2) load_stage<kOneRun>(st, w, min(t + 3, w.n - 1), min(t + 2, w.n - 1));
+    if (kMode != 2) {
 #pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-      const float e0 = __builtin_amdgcn_exp2f(a.s[kb][i]);
-      const float e1 = __builtin_amdgcn_exp2f(a.s[kb][i + 1]);
-      acc0 += e0;
-      acc1 += e1;
-      a.p[kb][i >> 3][i & 7] = (__bf16)e0;
-      a.p[kb][i >> 3][(i & 7) + 1] = (__bf16)e1;
+      for (int e = 0; e < 8; e += 2) {
+        const int kb = q >> 1, i = 8 * (q & 1) + e;
+        const float e0 = __builtin_amdgcn_exp2f(a.s[kb][i]);
+        const float e1 = __builtin_amdgcn_exp2f(a.s[kb][i + 1]);
+        acc0 += e0;
+        acc1 += e1;
+        a.p[kb][i >> 3][i & 7] = (__bf16)e0;
+        a.p[kb][i >> 3][(i & 7) + 1] = (__bf16)e1;
+      }
     }
+    __builtin_amdgcn_sched_barrier(0);
+  }
   a.l += acc0 + acc1;
 }
 
@@ -293,8 +305,7 @@ __device__ __forceinline__ void step(Acc& a, Stage& st, Walk& w, const Queries& 
   if (t >= w.n) return;
   if (!kIdle) m_phase<kFirst ? 1 : 0, (kFirst && kMode == 0) || kMode == 2>(a, kSlot, (kSlot + 2) % kRing, q, w);
   barrier();
-  turn_stage<kSlot, kOneRun>(st, w, t);
-  if (!kIdle) softmax<kMode, kFirst>(a, t, w);
+  v_phase<kMode, kSlot, kOneRun, kIdle, kFirst>(a, st, w, t);
   barrier();
 }
 
@@ -306,15 +317,13 @@ __device__ __forceinline__ void walk_begin(Stage& st, Walk& w) {
     w.vc = w.kc;
   }
   Stage second;
-  load_k<kOneRun>(st, w, 0);
-  load_v<kOneRun>(st, w, 0);
-  if (w.n > 1) load_k<kOneRun>(second, w, 1);
+  load_stage<kOneRun>(st, w, 0, 0);
+  load_stage<kOneRun>(second, w, min(1, w.n - 1), 0);
   __syncthreads();
   store_k(st, w, 0);
   store_v(st, w, 0);
-  if (w.n > 1) store_k(second, w, 1);
-  if (w.n > 2) load_k<kOneRun>(st, w, 2);
-  if (w.n > 1) load_v<kOneRun>(st, w, 1);
+  store_k(second, w, 1);
+  load_stage<kOneRun>(st, w, min(2, w.n - 1), min(1, w.n - 1));
 }
 
 template <int kMode, bool kOneRun, bool kIdle>
@@ -373,9 +382,10 @@ __global__ __launch_bounds__(kThreads) void mx8_attn_kernel(Mx8AttnArgs m) {
   {
     const int ts = tid & 7;
     w.lpiece = 16 * ts;
-    w.lscale = ts >> 1;
+    w.lshift = 8 * (ts >> 1);
+    w.lkey = ts == 0;
     w.wk = lds0 + w.lrow * kRow8 + (ts ^ swz8(w.lrow)) * 16;
-    w.ws = lds0 + kLdsS + w.lrow * kMxBlocks;
+    w.ws = lds0 + (ts == 0 ? kLdsS + w.lrow * kMxBlocks : kLdsDump + 4 * (tid & 63));
 #pragma unroll
     for (int i = 0; i < 2; ++i) w.wv[i] = lds0 + kLdsV + w.lrow * kRow16 + ((2 * ts + i) ^ swz16(w.lrow)) * 16;
   }
@@ -402,8 +412,7 @@ __global__ __launch_bounds__(kThreads) void mx8_attn_kernel(Mx8AttnArgs m) {
     const int64_t row0 = int64_t(bh) * a.slots;
     w.k8 = m.k8 + row0 * kRow8;
     w.v8 = m.v8 + row0 * kRow8;
-    w.ks = m.k_scale + row0 * kMxBlocks;
-    w.vs = m.v_scale + row0 * kMxBlocks;
+    w.lbase = (w.lkey ? m.k_scale : m.v_scale) + row0 * kMxBlocks;
     w.k_begin = sg.k0 * kBlockK;
     w.k_end = min(a.n_keys, sg.k1 * kBlockK);
     w.n = (w.k_end - w.k_begin + kBlockK - 1) / kBlockK;
