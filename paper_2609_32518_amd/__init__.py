@@ -39,9 +39,9 @@ if not os.path.exists(LIB_PATH):
                       "(there is no non-HIP fallback)")
 lib = ctypes.CDLL(LIB_PATH)
 try:
-    from . import _calls
+    from . import _calls, _calls_mx8
 except ImportError as e:
-    raise ImportError("the native module _calls is missing or does not load: build it with "
+    raise ImportError("the native modules _calls and _calls_mx8 are missing or do not load: build them with "
                       "`python paper_2609_32518_amd/build.py`") from e
 
 _i32, _i64, _f32, _f64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_double

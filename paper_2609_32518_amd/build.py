@@ -7,8 +7,9 @@ Run by path (not with -m): importing the package loads the library this script b
 Every source under csrc/ is compiled by hipcc to an object under _build/ and the
 objects are linked into paper_2609_32518_amd/libunstep.so, with ROCm's rocSOLVER and
 rocBLAS (the init-time SVD).  Device code is built
-with packed-fp32 instructions disabled.  native/calls.cpp, the binding's native calls, becomes
-paper_2609_32518_amd/_calls.so, a CPython extension module linked to torch and to libunstep.so.
+with packed-fp32 instructions disabled.  native/calls.cpp and native/calls_mx8.cpp, the binding's native
+calls, become paper_2609_32518_amd/_calls.so and _calls_mx8.so, CPython extension modules linked to torch
+and to libunstep.so.
 """
 from __future__ import annotations
 
@@ -27,6 +28,8 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libunstep.so")
 CALLS_SRC = os.path.join(PKG, "native", "calls.cpp")
 CALLS = os.path.join(PKG, "_calls.so")
+CALLS_MX8_SRC = os.path.join(PKG, "native", "calls_mx8.cpp")
+CALLS_MX8 = os.path.join(PKG, "_calls_mx8.so")
 
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 ARCH = "gfx950"
@@ -76,35 +79,35 @@ def _torch_dir() -> str:
     return os.path.dirname(importlib.util.find_spec("torch").origin)
 
 
-def _compile_calls(verbose: bool) -> str:
-    """The object of native/calls.cpp (host code only, against torch's headers)."""
+def _compile_calls(src: str, verbose: bool) -> str:
+    """The object of a native calls' source (host code only, against torch's headers)."""
     cxx = os.environ.get("CXX") or shutil.which("g++") or shutil.which("c++")
     if not cxx:
         raise RuntimeError("no C++ compiler found")
     inc = os.path.join(_torch_dir(), "include")
-    obj = os.path.join(BUILD, "calls.cpp.o")
+    obj = os.path.join(BUILD, os.path.basename(src) + ".o")
     _run([cxx, "-O2", "-std=c++17", "-fPIC", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM", f"-I{INCLUDE}", f"-isystem{inc}",
           f"-isystem{inc}/torch/csrc/api/include", f"-isystem{ROCM}/include",
-          f"-isystem{sysconfig.get_paths()['include']}", "-c", CALLS_SRC, "-o", obj], f"compiling {CALLS_SRC}", verbose)
+          f"-isystem{sysconfig.get_paths()['include']}", "-c", src, "-o", obj], f"compiling {src}", verbose)
     return obj
 
 
-def _link_calls(obj: str, verbose: bool) -> None:
+def _link_calls(obj: str, out: str, verbose: bool) -> None:
     cxx = os.environ.get("CXX") or shutil.which("g++") or shutil.which("c++")
     tl = os.path.join(_torch_dir(), "lib")
-    tmp = CALLS + ".tmp"
+    tmp = out + ".tmp"
     _run([cxx, "-shared", "-o", tmp, obj, f"-L{PKG}", "-lunstep", f"-L{tl}", "-ltorch_python", "-ltorch", "-ltorch_cpu",
-          "-lc10", "-lc10_hip", "-Wl,-z,now", "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{tl}"], "linking _calls.so", verbose)
-    os.replace(tmp, CALLS)
+          "-lc10", "-lc10_hip", "-Wl,-z,now", "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{tl}"], f"linking {os.path.basename(out)}", verbose)
+    os.replace(tmp, out)
 
 
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     srcs = sources()
-    with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, len(srcs) + 1)) as ex:
-        calls = ex.submit(_compile_calls, verbose)
+    with concurrent.futures.ThreadPoolExecutor(max_workers=min(8, len(srcs) + 2)) as ex:
+        calls = [ex.submit(_compile_calls, s, verbose) for s in (CALLS_SRC, CALLS_MX8_SRC)]
         objs = list(ex.map(lambda s: _compile(s, verbose), srcs))
-        calls_obj = calls.result()
+        calls_objs = [c.result() for c in calls]
     tmp = LIB + ".tmp"
     cmd = [hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp] + objs + [
         f"-L{ROCM}/lib", "-lrocsolver", "-lrocblas", f"-Wl,-rpath,{ROCM}/lib"]
@@ -114,7 +117,8 @@ def build(verbose: bool = False) -> str:
     if r.returncode != 0:
         raise RuntimeError(f"linking libunstep.so failed:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, LIB)
-    _link_calls(calls_obj, verbose)
+    for obj, out in zip(calls_objs, (CALLS, CALLS_MX8)):
+        _link_calls(obj, out, verbose)
     return LIB
 
 

@@ -7,7 +7,7 @@ from typing import Optional, Tuple
 
 import torch
 
-from . import HEAD_DIM, Cache, _check, _need, _ptr, _stream, _used_on, _vp, lib
+from . import HEAD_DIM, Cache, _calls_mx8, _check, _need, _ptr, _stream, _used_on, _vp, lib
 from .rotary import layout_code, norm_weights, table_rot
 
 E4M3 = torch.float8_e4m3fn
@@ -43,11 +43,16 @@ class CacheMX8:
                                            self.v8.data_ptr(), self.v_scale.data_ptr()))
         self.handle = h
         self._ws: Optional[torch.Tensor] = None
+        # the native calls' view of this cache; None: not on a GPU, or a subclass with its own checks or outputs
+        self._native = None
+        if all(getattr(type(self), f.__name__) is f for f in _CHECK_METHODS):
+            self._native = _calls_mx8.cache(h.value, self.B, self.H, self.T, self.k8, _SCRATCH_METHODS)
 
-    def __del__(self):
+    def __del__(self, _destroy=lib.unstep_cache_destroy):
+        self._native = None                # it holds the handle's address
         h = getattr(self, "handle", None)
         if h is not None and h.value:
-            lib.unstep_cache_destroy(h)
+            _destroy(h)
             self.handle = None
 
     # -- host index state and checks: those of Cache ----------------------------------
@@ -90,6 +95,11 @@ class CacheMX8:
                              stream=None) -> Optional[Tuple[torch.Tensor, torch.Tensor]]:
         """Rotate and quantise the chunk's keys and values into the cache; returns the quantised queries
         (q8, q_scale), which hold the softmax scale, or None without q."""
+        if stream is None and self._native is not None:
+            r = _calls_mx8.append_mx8(self._native, start_frame, n_frames, q, k, v, cos_t, sin_t, layout, q_norm_weight,
+                                      k_norm_weight, norm_eps, softmax_scale, q8, q_scale)
+            if r is not None:
+                return r[0]
         ts, hs = self._qkv_strides(q, k, v, n_frames)
         rot, code = table_rot(self, cos_t, sin_t, n_frames), layout_code(layout)
         norm_weights(self, q, q_norm_weight, k_norm_weight)
@@ -107,6 +117,11 @@ class CacheMX8:
                                q_scale: torch.Tensor, out: Optional[torch.Tensor] = None,
                                lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                                use_split: bool = True, stream=None) -> torch.Tensor:
+        if stream is None and self._native is not None:
+            r = _calls_mx8.window_attn_mx8(self._native, start_frame, n_frames, window_frames, q8, q_scale, out, lse,
+                                           workspace, use_split, self)
+            if r is not None:
+                return r
         q8, q_scale = self._queries(q8, q_scale, n_frames, False)
         out = self._chunk_out(out, "out", n_frames)
         self._lse(lse, n_frames)
@@ -127,6 +142,12 @@ class CacheMX8:
                         lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                         use_split: bool = True, stream=None) -> torch.Tensor:
         """unstep_kv_append_mx8 and unstep_window_attn_mx8 in one call."""
+        if stream is None and self._native is not None:
+            r = _calls_mx8.step_mx8(self._native, start_frame, n_frames, q, k, v, cos_t, sin_t, window_frames, layout,
+                                    q_norm_weight, k_norm_weight, norm_eps, softmax_scale, q8, q_scale, out, lse, workspace,
+                                    use_split, self)
+            if r is not None:
+                return r
         if q is None:
             raise ValueError("unstep_step_mx8 needs q")
         ts, hs = self._qkv_strides(q, k, v, n_frames)
@@ -149,6 +170,10 @@ class CacheMX8:
     def unstep_kv_read_mx8(self, start_frame: int, n_frames: int, k_out: Optional[torch.Tensor] = None,
                            v_out: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
         """The frames' rotated keys and values as bf16 [B, N, H, 128], exact."""
+        if stream is None and self._native is not None:
+            r = _calls_mx8.read_mx8(self._native, start_frame, n_frames, k_out, v_out)
+            if r is not None:
+                return r
         n = max(0, n_frames)
         k_out, v_out = self._chunk_out(k_out, "k_out", n), self._chunk_out(v_out, "v_out", n)
         with torch.cuda.device(self.device):
@@ -158,10 +183,19 @@ class CacheMX8:
         return k_out, v_out
 
 
+_CHECK_METHODS = (CacheMX8._strides, CacheMX8._qkv_strides, CacheMX8._chunk_out, CacheMX8._lse, CacheMX8._workspace_bytes,
+                  CacheMX8._queries)
+_SCRATCH_METHODS = (CacheMX8.workspace, CacheMX8.workspace_bytes, CacheMX8.workspace)
+
+
 def unstep_mx8_dequantize(x8: torch.Tensor, scale: torch.Tensor, out: Optional[torch.Tensor] = None,
                           stream=None) -> torch.Tensor:
     """bf16 values of quantised rows x8 [..., 128] (e4m3) with scale bytes [..., 4], exact for what the
     quantising append writes."""
+    if stream is None:
+        r = _calls_mx8.dequantize(x8, scale, out)
+        if r is not None:
+            return r
     if x8.dim() < 1 or x8.shape[-1] != HEAD_DIM:
         raise ValueError("x8 must have shape [..., 128]")
     _need(x8, "x8", tuple(x8.shape), E4M3, x8.device)

@@ -7,7 +7,7 @@ from typing import Optional, Tuple
 
 import torch
 
-from . import HEAD_DIM, _check, _need, _ptr, _stream, _used_on, lib
+from . import HEAD_DIM, _calls_mx8, _check, _need, _ptr, _stream, _used_on, lib
 
 ROTARY_LAYOUTS = {"interleaved": 0, "half": 1}
 ROTARY_SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}
@@ -32,6 +32,11 @@ def unstep_rotary_tables(start_frame: int, n_frames: int, grid_h: int, grid_w: i
     if scaling not in ROTARY_SCALINGS:
         raise ValueError(f"unknown scaling {scaling!r}")
     d_t, d_h, d_w = dims
+    if out is None and stream is None and device == "cuda" and torch.cuda.is_initialized():
+        r = _calls_mx8.tables(start_frame, n_frames, grid_h, grid_w, d_t, d_h, d_w, theta, ROTARY_SCALINGS[scaling], factor,
+                              trained_frames, *turns, amplitude)
+        if r is not None:
+            return r
     opt = _Rotary(d_t, d_h, d_w, ROTARY_SCALINGS[scaling], theta, factor, trained_frames, turns[0], turns[1], amplitude)
     shape = (max(0, n_frames) * max(0, grid_h) * max(0, grid_w), max(0, sum(dims)) // 2)
     if out is None:
@@ -73,6 +78,10 @@ def norm_weights(cache, q, wq, wk) -> None:
 
 
 def append_rotary(cache, start_frame, n_frames, q, k, v, cos_t, sin_t, layout, wq, wk, eps, q_rot, stream):
+    if stream is None and cache._native is not None:
+        r = _calls_mx8.append_rotary(cache._native, start_frame, n_frames, q, k, v, cos_t, sin_t, layout, wq, wk, eps, q_rot)
+        if r is not None:
+            return r[0]
     ts, hs = cache._qkv_strides(q, k, v, n_frames)
     rot, code = table_rot(cache, cos_t, sin_t, n_frames), layout_code(layout)
     norm_weights(cache, q, wq, wk)
