@@ -75,6 +75,8 @@ int plan_rotary(const unstep_cache* c, int32_t layout, int32_t rot, bool with_q,
     return fail(UNSTEP_E_RANGE, "%s: unknown layout %d", where, layout);
   if (rot < 16 || rot > UNSTEP_HEAD_DIM || rot % 16)
     return fail(UNSTEP_E_SHAPE, "%s: rot_dim %d must be a multiple of 16 up to 128", where, rot);
+  if (p->args.tok_stride > UINT32_MAX || p->args.head_stride > UINT32_MAX)
+    return fail(UNSTEP_E_SHAPE, "%s: strides above 2^32 elements", where);
   // the pass numbers the 16-byte pieces of one batch's chunk in 32 bits
   if (int64_t(p->args.C) * p->args.T * c->H * (UNSTEP_HEAD_DIM / 8) > INT32_MAX)
     return fail(UNSTEP_E_SHAPE, "%s: too many tokens x heads in one chunk", where);

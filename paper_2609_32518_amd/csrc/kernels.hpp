@@ -39,6 +39,18 @@ constexpr int kNormMaxHeads = 32;
 
 hipError_t launch_rope_append(const RopeAppendArgs& a, hipStream_t stream);
 
+// n / d for n < 2^31 by one multiplication: the launch knows the divisors, the kernel's own division is
+// a dozen instructions, three of them multiplications.
+struct FastDiv {
+  uint32_t mul, shift;
+};
+inline FastDiv fast_div(uint32_t d) {
+  // mul = ceil(2^(31 + s) / d) with 2^s >= d: the error n (mul d - 2^(31 + s)) / (d 2^(31 + s)) stays below 1 / d
+  uint32_t s = 0;
+  while ((uint64_t(1) << s) < d) ++s;
+  return FastDiv{uint32_t(((uint64_t(1) << (31 + s)) + d - 1) / d), s};
+}
+
 // The rotating append with its options: interleaved or half layout over the first `rot` dimensions of a
 // head, and either a bf16 cache or a quantised one.
 struct RotaryAppendArgs {
@@ -49,6 +61,9 @@ struct RotaryAppendArgs {
   // the places of q_rot, k_cache and v_cache
   uint8_t *q8, *q_scale, *k8, *k_scale, *v8, *v_scale;
   float q_mul;             // the quantised queries' factor
+  // set by the launcher: divisions by heads, tokens per frame, ring frames; 1 / channels
+  FastDiv by_h, by_t, by_r;
+  double inv_channels;
 };
 hipError_t launch_rotary_append(const RotaryAppendArgs& a, hipStream_t stream);
 

@@ -19,12 +19,10 @@ constexpr int kMxBlocks = 4;             // per row of 128
 constexpr int32_t kMxMinByte = 27;       // 2^-100
 
 // The scale byte of a block from the bits of its largest finite |y|: 1.f 2^k takes k - 8 where
-// 1.f <= 1.75 = 448 / 256, else k - 7.
+// 1.f <= 1.75 = 448 / 256, else k - 7 (the sum carries into the exponent).
 __device__ __forceinline__ int32_t mx8_byte(uint32_t top) {
-  const int32_t b = int32_t(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
-  return max(b, kMxMinByte);
+  return max(int32_t((top + 0x1fffffu) >> 23) - 8, kMxMinByte);
 }
-__device__ __forceinline__ float mx8_inverse(int32_t byte) { return __uint_as_float(uint32_t(254 - byte) << 23); }
 __device__ __forceinline__ float mx8_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 }  // namespace unstep

@@ -23,14 +23,12 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kPieces = kHeadDim / 8;   // pieces of a head vector, one lane each
-// pieces per lane of the normalising kernel (a wave per token): 3 cover 12 heads, 8 cover kNormMaxHeads
-constexpr int kNormPiecesSmall = 3;
-constexpr int kNormPiecesLarge = kNormMaxHeads * kPieces / 64;
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef short i16x2_t __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
@@ -47,6 +45,11 @@ __device__ __forceinline__ F8 widen(u32x4_t x) {
     y.v[2 * e + 1] = bf16_hi(x[e]);
   }
   return y;
+}
+
+template <int kCtrl>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) {
+  return uint32_t(__builtin_amdgcn_update_dpp(0, int(x), kCtrl, 0xf, 0xf, false));
 }
 
 // What a piece needs of its token's tables: 4 entries of cos and of sin (interleaved) or 8 (half).
@@ -80,8 +83,13 @@ __device__ __forceinline__ F8 rotate(u32x4_t x, const Turn<kHalf>& t, const Rota
     const int lane = threadIdx.x & 63;
     const int from = p >= 2 * hp ? lane : p >= hp ? lane - hp : lane + hp;
     u32x4_t o;
+    if (r.rot == kHeadDim) {                              // the whole head: 8 lanes on or back within the 16
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = uint32_t(__shfl(int(x[e]), from));
+      for (int e = 0; e < 4; ++e) o[e] = dpp<0x128>(x[e]);   // row_ror 8
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = uint32_t(__shfl(int(x[e]), from));
+    }
     const F8 other = widen(o);
     if (p < 2 * hp) {
       // first half: x_a c - x_b s, second: x_b c + x_a s (= x_a s + x_b c, addition commutes)
@@ -117,36 +125,36 @@ __device__ __forceinline__ u32x4_t to_bf16(const F8& y) {
   return o;
 }
 
-template <int kCtrl>
-__device__ __forceinline__ uint32_t dpp(uint32_t x) {
-  return uint32_t(__builtin_amdgcn_update_dpp(0, int(x), kCtrl, 0xf, 0xf, false));
-}
-
-// Stores piece p of the head vector at row `row`: eight e4m3 bytes, and (lane of piece 0) the row's
-// scale bytes.  The 16 lanes of the vector are in this together.
-__device__ __forceinline__ void store_mx8(const F8& y, uint8_t* x8, uint8_t* scale, int64_t row, int32_t p) {
-  uint32_t top = 0;
+// The scale byte of the block (4 lanes) that this lane's 8 values belong to.  Magnitudes compare as
+// integers; a value that is not finite, which does not count, sends the lane through its values again.
+__device__ __forceinline__ int32_t block_byte(const F8& y) {
+  uint32_t m[8], top = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t m = __float_as_uint(y.v[i]) & 0x7fffffffu;
-    top = max(top, m < 0x7f800000u ? m : 0u);
+  for (int i = 0; i < 8; ++i) m[i] = __float_as_uint(y.v[i]) & 0x7fffffffu;
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) top = max(max(m[i], m[i + 1]), top);
+  if (__builtin_expect(top >= 0x7f800000u, 0)) {
+    top = 0;
+    for (int i = 0; i < 8; ++i) top = m[i] < 0x7f800000u ? max(top, m[i]) : top;
   }
   top = max(top, dpp<0xb1>(top));                         // quad_perm 1,0,3,2
   top = max(top, dpp<0x4e>(top));                         // quad_perm 2,3,0,1
-  const int32_t byte = mx8_byte(top);
-  const float inv = mx8_inverse(byte);
-  float z[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t m = __float_as_uint(y.v[i]) & 0x7fffffffu;
-    z[i] = m < 0x7f800000u ? y.v[i] * inv : __uint_as_float(0x7fc00000u);
-  }
+  return mx8_byte(top);
+}
+
+// Stores piece p of the head vector at row `row`: eight e4m3 bytes (the conversion divides by the power of
+// two and rounds once; infinities become NaN), and (lane of piece 0) the row's scale bytes.  The 16 lanes of the
+// vector are in this together.
+__device__ __forceinline__ void store_mx8(const F8& y, uint8_t* x8, uint8_t* scale, int64_t row, int32_t p) {
+  const int32_t byte = block_byte(y);
+  const float s = mx8_scale(uint32_t(byte));
   u32x2_t w;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    int d = __builtin_amdgcn_cvt_pk_fp8_f32(z[4 * i], z[4 * i + 1], 0, false);
-    d = __builtin_amdgcn_cvt_pk_fp8_f32(z[4 * i + 2], z[4 * i + 3], d, true);
-    w[i] = uint32_t(d);
+    i16x2_t d = {};
+    d = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(d, y.v[4 * i], y.v[4 * i + 1], s, false);
+    d = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(d, y.v[4 * i + 2], y.v[4 * i + 3], s, true);
+    w[i] = __builtin_bit_cast(uint32_t, d);
   }
   __builtin_nontemporal_store(w, reinterpret_cast<u32x2_t*>(x8 + row * kHeadDim + p * 8));
   uint32_t bytes = uint32_t(byte) << (8 * (p >> 2));
@@ -155,15 +163,27 @@ __device__ __forceinline__ void store_mx8(const F8& y, uint8_t* x8, uint8_t* sca
   if (p == 0) *reinterpret_cast<uint32_t*>(scale + row * kMxBlocks) = bytes;
 }
 
+__device__ __forceinline__ uint32_t divide(uint32_t n, FastDiv d) {
+  return uint32_t((uint64_t(n) * d.mul) >> 31) >> d.shift;
+}
+
 // Places of token n of batch b, head h: row of the chunk's outputs, and of the cache.
 struct Place {
   int64_t chunk_row, cache_row;
 };
-__device__ __forceinline__ Place place(const RopeAppendArgs& a, int32_t b, int32_t n, int32_t h) {
-  const int32_t fi = n / a.T, t = n - fi * a.T;
-  const int32_t slot = frame_slot(a.f0 + fi, a.S, a.R);
-  return Place{(int64_t(b) * (int64_t(a.C) * a.T) + n) * a.H + h,
-               (int64_t(b) * a.H + h) * a.slots + int64_t(slot) * a.T + t};
+__device__ __forceinline__ Place place(const RotaryAppendArgs& r, int32_t b, uint32_t n, uint32_t h) {
+  const RopeAppendArgs& a = r.a;
+  const uint32_t fi = divide(n, r.by_t), t = n - fi * uint32_t(a.T);
+  const int32_t f = a.f0 + int32_t(fi), g = f - a.S;       // frame, and which of the ring's
+  const uint32_t slot = g < 0 ? uint32_t(f) : uint32_t(a.S) + uint32_t(g) - divide(uint32_t(g), r.by_r) * uint32_t(a.R);
+  const uint32_t N = uint32_t(a.C) * uint32_t(a.T);
+  return Place{int64_t(b) * N * a.H + (n * uint32_t(a.H) + h),
+               int64_t(b) * a.H * a.slots + int64_t(uint64_t(h) * uint32_t(a.slots) + (slot * uint32_t(a.T) + t))};
+}
+// Element offset of piece p of token n, head h in the inputs of batch b.
+__device__ __forceinline__ int64_t source(const RopeAppendArgs& a, int32_t b, uint32_t n, uint32_t h, uint32_t p) {
+  const uint32_t N = uint32_t(a.C) * uint32_t(a.T);
+  return int64_t(b) * N * a.tok_stride + int64_t(uint64_t(n) * uint32_t(a.tok_stride) + uint64_t(h) * uint32_t(a.head_stride) + p * 8);
 }
 
 template <bool kHalf, bool kMx8, bool kQuery>
@@ -198,108 +218,160 @@ __global__ __launch_bounds__(kThreads) void rotary_append_kernel(RotaryAppendArg
   const uint32_t hv = u / kPieces;                        // (token, head) of the chunk
   if (hv >= uint32_t(a.C) * a.T * a.H) return;            // whole head vectors: 16 lanes each
   const int32_t p = u % kPieces;
-  const int32_t n = hv / uint32_t(a.H), h = hv - uint32_t(n) * a.H;
+  const uint32_t n = divide(hv, r.by_h), h = hv - n * uint32_t(a.H);
   const int32_t b = blockIdx.y;
-  const int64_t src = (int64_t(b) * (int64_t(a.C) * a.T) + n) * a.tok_stride + int64_t(h) * a.head_stride + p * 8;
+  const int64_t src = source(a, b, n, h, p);
   const u32x4_t kx = *reinterpret_cast<const u32x4_t*>(a.k + src);
   const u32x4_t vx = *reinterpret_cast<const u32x4_t*>(a.v + src);
   u32x4_t qx = {};
   if (kWithQ) qx = *reinterpret_cast<const u32x4_t*>(a.q + src);
   const Turn<kHalf> t = load_turn<kHalf>(r, n, p);
-  const Place at = place(a, b, n, h);
+  const Place at = place(r, b, n, h);
   put_rotated<kHalf, kMx8, false>(r, rotate<kHalf>(kx, t, r, p), at, p);
   put_value<kMx8>(r, vx, at, p);
   if (kWithQ) put_rotated<kHalf, kMx8, true>(r, rotate<kHalf>(qx, t, r, p), at, p);
 }
 
-// ---- with the RMS normalisation: one wave per token, lane l owning the pieces l, l + 64, ... of its heads.
-// x'_j = bf16(fp32((x_j rr) w_j)), rr = 1 / sqrt(sum x^2 / channels + eps) in fp64 (each bf16 square is exact).
-template <int kPer>
-__device__ __forceinline__ double sum_sq(const u32x4_t (&x)[kPer], int n) {
+// ---- with the RMS normalisation: a token's head vectors on ceil(heads / 4) waves, one piece per lane as above.
+// x'_j = bf16(fp32(x_j r w_j)), r = 1 / sqrt(sum x^2 / channels + eps) in fp64 (each bf16 square is exact), summed
+// over a wave by exchanges and over the token's waves through LDS, in one order.
+// What bounds it is arithmetic beside the memory traffic: 4680 tokens x 12 heads take 15.8 us into the quantised
+// cache (67.7 MB; 12.5 without the normalisation, the rate of a copy) and 15.1 into the bf16 one (88.7 MB; 14.3).
+// Before: fp64 products per channel and a wave per token 21.4; binary32 pairs 17.5; one piece per lane,
+// divisions by multiplication and two Newton steps for the root 16.0; 64 registers, so that 8 waves fit a
+// SIMD, and the values stored before the statistic is known 15.8.
+__device__ __forceinline__ double sum_sq(u32x4_t x) {
   double s = 0.0;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    if (i >= n) break;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const double lo = bf16_lo(x[i][e]), hi = bf16_hi(x[i][e]);
-      s += lo * lo;
-      s += hi * hi;
-    }
+  for (int e = 0; e < 4; ++e) {
+    const double lo = bf16_lo(x[e]), hi = bf16_hi(x[e]);
+    s += lo * lo;
+    s += hi * hi;
   }
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off);
   return s;
 }
 
-// The binary32 value is kept opaque to the optimiser, which would fold the two roundings into one.
-__device__ __forceinline__ u32x4_t normalise8(u32x4_t x, u32x4_t w, double rr) {
-  u32x4_t y;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    float lo = (float)(((double)bf16_lo(x[e]) * rr) * (double)bf16_lo(w[e]));
-    float hi = (float)(((double)bf16_hi(x[e]) * rr) * (double)bf16_hi(w[e]));
-    asm volatile("" : "+v"(lo), "+v"(hi));
-    bf16x2_t pr;
-    pr[0] = (__bf16)lo;
-    pr[1] = (__bf16)hi;
-    y[e] = __builtin_bit_cast(uint32_t, pr);
-  }
-  return y;
+// 1 / sqrt(x), as it is and as a sum of two binary32 numbers.
+struct Rms {
+  float hi, lo;
+  double r;
+  bool plain;                                             // 2^-51 < r < 2^51, the same for the whole wave
+};
+// The binary32 reciprocal root (2^-22) and two Newton steps in fp64 for ordinary x: within two units of the
+// last place of fp64, for a quarter of the instructions of the square root and division.
+__device__ __forceinline__ double inverse_root(double x) {
+  if (__builtin_expect(!(x > 0x1p-100 && x < 0x1p100), 0)) return 1.0 / sqrt(x);
+  double y = (double)__builtin_amdgcn_rsqf((float)x);
+  const double h = 0.5 * x;
+  y = y * (1.5 - h * y * y);
+  return y * (1.5 - h * y * y);
+}
+__device__ __forceinline__ double lane_value(double v, int lane) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane(uint32_t(u), lane), hi = __builtin_amdgcn_readlane(uint32_t(u >> 32), lane);
+  return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
+}
+__device__ __forceinline__ Rms rms_of(double r) {
+  Rms m;
+  m.r = r;
+  m.hi = (float)r;
+  m.lo = (float)(r - (double)m.hi);
+  m.plain = r > 0x1p-51 && r < 0x1p51;
+  return m;
+}
+template <int kCtrl>
+__device__ __forceinline__ double dpp(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  return __builtin_bit_cast(double, uint64_t(dpp<kCtrl>(uint32_t(u >> 32))) << 32 | dpp<kCtrl>(uint32_t(u)));
+}
+// Both sums of a wave in one reduction: its lower half takes the keys', the upper the queries', so that the
+// steps after the first, and the root later, are done once for the two.
+__device__ __forceinline__ double wave_sums(double k, double q) {
+  const bool upper = (threadIdx.x & 32) != 0;
+  double s = (upper ? q : k) + __shfl_xor(upper ? k : q, 32);
+  s += dpp<0xb1>(s);                                      // quad_perm 1,0,3,2
+  s += dpp<0x4e>(s);                                      // quad_perm 2,3,0,1
+  s += dpp<0x141>(s);                                     // row_half_mirror: the other quad of 8
+  s += dpp<0x140>(s);                                     // row_mirror: the other 8 of 16
+  return s + __shfl_xor(s, 16);
 }
 
-template <bool kWithQ, bool kHalf, bool kMx8, int kPer>
-__global__ __launch_bounds__(kThreads) void rotary_norm_append_kernel(RotaryAppendArgs r) {
-  const RopeAppendArgs& a = r.a;
-  const int32_t N = a.C * a.T;
-  const int32_t n = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-  if (n >= N) return;                                     // whole wave
-  const int lane = threadIdx.x & 63;
-  const int b = blockIdx.y;
-  const int32_t pieces = a.H * kPieces;
-  const int np = (pieces - lane + 63) / 64;               // the same for the 16 lanes of a head vector
-  const int32_t p = lane % kPieces;
-  u32x4_t kx[kPer], vx[kPer], qx[kPer];
+// bf16(fp32(x r w)) for the 8 channels of a piece.  x w is exact in binary32 (8 and 8 bits); its product with
+// hi + lo, formed as p + (its error + x w lo), is within 2^-47 of the exact one before its only rounding to
+// binary32, as the fp64 product is within 2^-52: four binary32 operations instead of five conversions and
+// products in fp64, which the pass's time went into.  The binary32 value is kept opaque, or the two roundings
+// would be folded into one.
+__device__ __forceinline__ u32x4_t normalise8(u32x4_t x, u32x4_t w, const Rms& m) {
+#pragma clang fp contract(off)
+  const F8 xs = widen(x), ws = widen(w);
+  F8 v;
+  if (__builtin_expect(m.plain, 1)) {
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    if (i >= np) break;
-    const int32_t h = (lane + 64 * i) / kPieces;
-    const int64_t src = (int64_t(b) * N + n) * a.tok_stride + int64_t(h) * a.head_stride + p * 8;
-    kx[i] = *reinterpret_cast<const u32x4_t*>(a.k + src);
-    vx[i] = *reinterpret_cast<const u32x4_t*>(a.v + src);
-    if (kWithQ) qx[i] = *reinterpret_cast<const u32x4_t*>(a.q + src);
-  }
-  const Turn<kHalf> t = load_turn<kHalf>(r, n, p);
-  const double inv_c = 1.0 / double(a.H * kHeadDim);
-  const double rk = 1.0 / sqrt(sum_sq(kx, np) * inv_c + a.eps);
-  double rq = 0.0;
-  if (kWithQ) rq = 1.0 / sqrt(sum_sq(qx, np) * inv_c + a.eps);
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    if (i >= np) break;
-    const int32_t h = (lane + 64 * i) / kPieces;
-    const Place at = place(a, b, n, h);
-    const int32_t ch = h * kHeadDim + p * 8;
-    const u32x4_t wk = *reinterpret_cast<const u32x4_t*>(a.wk + ch);
-    put_rotated<kHalf, kMx8, false>(r, rotate<kHalf>(normalise8(kx[i], wk, rk), t, r, p), at, p);
-    put_value<kMx8>(r, vx[i], at, p);
-    if (kWithQ) {
-      const u32x4_t wq = *reinterpret_cast<const u32x4_t*>(a.wq + ch);
-      put_rotated<kHalf, kMx8, true>(r, rotate<kHalf>(normalise8(qx[i], wq, rq), t, r, p), at, p);
+    for (int i = 0; i < 8; ++i) {
+      const float t = xs.v[i] * ws.v[i];
+      const float p = t * m.hi;
+      v.v[i] = p + __builtin_fmaf(t, m.lo, __builtin_fmaf(t, m.hi, -p));
     }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v.v[i] = (float)(((double)xs.v[i] * m.r) * (double)ws.v[i]);
   }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(v.v[i]));
+  return to_bf16(v);
+}
+
+constexpr int kNormMaxWaves = kNormMaxHeads * kPieces / 64;   // of a token, and of a work-group
+static_assert(kNormMaxWaves == 8, "");
+
+template <bool kWithQ, bool kHalf, bool kMx8>
+__global__ __launch_bounds__(kNormMaxWaves * 64, 8) void rotary_norm_append_kernel(RotaryAppendArgs r, int32_t waves) {
+  const RopeAppendArgs& a = r.a;
+  __shared__ double sums[kNormMaxWaves][2];
+  const int32_t N = a.C * a.T;
+  const int lane = threadIdx.x & 63;
+  const int32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int32_t tok = wave / waves, part = wave - tok * waves;               // of the work-group; wave of the token
+  const int32_t n = blockIdx.x * (int32_t(blockDim.x >> 6) / waves) + tok;
+  const int32_t b = blockIdx.y;
+  const int32_t h = 4 * part + (lane >> 4), p = lane % kPieces;
+  const bool here = n < N && h < a.H;                                        // the same for a head vector's 16 lanes
+  u32x4_t kx = {}, vx = {}, qx = {}, wk = {}, wq = {};
+  Turn<kHalf> t{};
+  if (here) {
+    const int64_t src = source(a, b, n, h, p);
+    kx = *reinterpret_cast<const u32x4_t*>(a.k + src);
+    if (kWithQ) qx = *reinterpret_cast<const u32x4_t*>(a.q + src);
+    t = load_turn<kHalf>(r, n, p);
+    vx = *reinterpret_cast<const u32x4_t*>(a.v + src);
+    wk = *reinterpret_cast<const u32x4_t*>(a.wk + h * kHeadDim + p * 8);
+    if (kWithQ) wq = *reinterpret_cast<const u32x4_t*>(a.wq + h * kHeadDim + p * 8);
+  }
+  const double s = wave_sums(sum_sq(kx), kWithQ ? sum_sq(qx) : 0.0);
+  if ((lane & 31) == 0) sums[wave][lane >> 5] = s;
+  Place at{};
+  if (here) {                                             // the values need no statistic
+    at = place(r, b, n, h);
+    put_value<kMx8>(r, vx, at, p);
+  }
+  __syncthreads();
+  double ss = 0.0;
+  for (int32_t i = 0; i < waves; ++i) ss += sums[tok * waves + i][lane >> 5];
+  const double rr = inverse_root(ss * r.inv_channels + a.eps);
+  const Rms rk = rms_of(lane_value(rr, 0)), rq = rms_of(lane_value(rr, 32));
+  if (!here) return;
+  put_rotated<kHalf, kMx8, false>(r, rotate<kHalf>(normalise8(kx, wk, rk), t, r, p), at, p);
+  if (kWithQ) put_rotated<kHalf, kMx8, true>(r, rotate<kHalf>(normalise8(qx, wq, rq), t, r, p), at, p);
 }
 
 template <bool kWithQ, bool kHalf, bool kMx8>
 void launch(const RotaryAppendArgs& r, hipStream_t stream) {
   const RopeAppendArgs& a = r.a;
   if (a.wk) {
-    const int32_t N = a.C * a.T;
-    const dim3 grid(unsigned((N + kThreads / 64 - 1) / (kThreads / 64)), unsigned(a.B));
-    if (a.H * kPieces <= 64 * kNormPiecesSmall)
-      hipLaunchKernelGGL((rotary_norm_append_kernel<kWithQ, kHalf, kMx8, kNormPiecesSmall>), grid, dim3(kThreads), 0, stream, r);
-    else
-      hipLaunchKernelGGL((rotary_norm_append_kernel<kWithQ, kHalf, kMx8, kNormPiecesLarge>), grid, dim3(kThreads), 0, stream, r);
+    const int32_t waves = (a.H + 3) / 4, tokens = waves < 4 ? 4 / waves : 1;  // of a token; tokens of a work-group
+    const dim3 grid(unsigned((a.C * a.T + tokens - 1) / tokens), unsigned(a.B));
+    hipLaunchKernelGGL((rotary_norm_append_kernel<kWithQ, kHalf, kMx8>), grid, dim3(unsigned(waves * tokens * 64)), 0, stream, r,
+                       waves);
     return;
   }
   const int64_t units = int64_t(a.C) * a.T * a.H * kPieces;
@@ -314,7 +386,12 @@ void launch(const RotaryAppendArgs& r, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_rotary_append(const RotaryAppendArgs& r, hipStream_t stream) {
+hipError_t launch_rotary_append(const RotaryAppendArgs& args, hipStream_t stream) {
+  RotaryAppendArgs r = args;
+  r.by_h = fast_div(uint32_t(r.a.H));
+  r.by_t = fast_div(uint32_t(r.a.T));
+  r.by_r = fast_div(uint32_t(r.a.R));
+  r.inv_channels = 1.0 / double(r.a.H * kHeadDim);
   if (r.k8)
     r.half ? launch<true, true>(r, stream) : launch<false, true>(r, stream);
   else

@@ -214,3 +214,22 @@ def test_append_replayed_from_a_graph_and_on_another_stream():
         torch.cuda.synchronize()
         for x, y in ((a.k8, b.k8), (a.v8, b.v8), (a.k_scale, b.k_scale), (a.v_scale, b.v_scale), (q8, w8), (qs, ws)):
             assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+@pytest.mark.parametrize("scale,eps", [(2.0 ** 60, 0.0), (2.0 ** -62, 0.0), (2.0 ** 55, 1e-6), (2.0 ** -40, 1e-6), (2.0 ** -70, 0.0)])
+def test_normalisation_of_very_large_and_small_tokens(scale, eps):
+    """Statistics outside the range of the fast path, beside ordinary ones in the same work-group."""
+    B, H, gh, gw = 1, 3, 2, 4
+    g = np.random.default_rng(11)
+    x = g.standard_normal((B, gh * gw, H, 128))
+    x[:, 1::2] *= scale
+    bits = [f32_to_bf16_bits(x), f32_to_bf16_bits(x[:, ::-1]), f32_to_bf16_bits(x)]
+    c, s = (np.ascontiguousarray(t, np.float32) for t in mx8.tables(0, 1, gh, gw, (44, 42, 42)))
+    w, wd = weights(H, 5)
+    flat = lambda t: t.reshape(B, gh * gw, H * 128)  # noqa: E731
+    want = [mx8.rotate(rmsnorm.rms_norm_bf16(flat(bits[i]), w[i], eps).reshape(x.shape), c, s, False) for i in range(2)]
+    b = u.Cache(B, H, gh, gw, 0, 1)
+    q = b.unstep_kv_append_rotary(0, 1, *(dev(t) for t in bits), torch.from_numpy(c).cuda(), torch.from_numpy(s).cuda(),
+                                  q_norm_weight=wd[0], k_norm_weight=wd[1], norm_eps=eps)
+    assert np.array_equal(host(q), f32_to_bf16_bits(want[0]))
+    assert np.array_equal(host(b.k), f32_to_bf16_bits(want[1]).transpose(0, 2, 1, 3))
