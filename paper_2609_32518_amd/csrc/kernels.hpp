@@ -50,6 +50,7 @@ inline FastDiv fast_div(uint32_t d) {
   while ((uint64_t(1) << s) < d) ++s;
   return FastDiv{uint32_t(((uint64_t(1) << (31 + s)) + d - 1) / d), s};
 }
+__host__ __device__ inline uint32_t divide(uint32_t n, FastDiv d) { return uint32_t((uint64_t(n) * d.mul) >> 31) >> d.shift; }
 
 // The rotating append with its options: interleaved or half layout over the first `rot` dimensions of a
 // head, and either a bf16 cache or a quantised one.
@@ -88,6 +89,7 @@ struct Mx8ReadArgs {
   int32_t B, H, T, C, slots, f0, S, R;
   const uint8_t *y8, *y_scale;   // a second tensor of the same places into y_out, or null
   uint16_t* y_out;
+  FastDiv by_h, by_t, by_c, by_r;   // set by the launcher
 };
 hipError_t launch_mx8_read(const Mx8ReadArgs& a, hipStream_t stream);
 

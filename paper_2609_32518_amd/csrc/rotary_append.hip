@@ -163,10 +163,6 @@ __device__ __forceinline__ void store_mx8(const F8& y, uint8_t* x8, uint8_t* sca
   if (p == 0) *reinterpret_cast<uint32_t*>(scale + row * kMxBlocks) = bytes;
 }
 
-__device__ __forceinline__ uint32_t divide(uint32_t n, FastDiv d) {
-  return uint32_t((uint64_t(n) * d.mul) >> 31) >> d.shift;
-}
-
 // Places of token n of batch b, head h: row of the chunk's outputs, and of the cache.
 struct Place {
   int64_t chunk_row, cache_row;
