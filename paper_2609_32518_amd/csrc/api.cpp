@@ -205,7 +205,7 @@ int unstep_attn_workspace_size(const unstep_cache* c, int32_t start_frame, int32
     int rc = c->idx.retained_count(start_frame, n_frames, window_frames, &frames, &why);
     if (rc != UNSTEP_OK) return fail_msg(rc, "unstep_attn_workspace_size", why);
     const int32_t N = n_frames * c->idx.T();
-    *bytes = unstep::attn_plan(c->B, c->H, N, frames * c->idx.T()).workspace;
+    *bytes = (c->mx8() ? unstep::attn_plan_mx8 : unstep::attn_plan)(c->B, c->H, N, frames * c->idx.T(), unstep::kAttnMaxWorkspace).workspace;
     return ok();
   });
 }

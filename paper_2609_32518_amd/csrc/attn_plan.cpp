@@ -79,4 +79,21 @@ AttnPlan attn_plan(int32_t B, int32_t H, int32_t N, int32_t n_keys, size_t scrat
   return plan_of(B, H, N, n_keys, int64_t(scratch / attn_workspace_bytes(1)));
 }
 
+// Few queries: equal parts of a (batch, head)'s keys, one work-group each.  A work-group takes 256 keys (four
+// tiles) at a time, 1.33 us a round, and a merge costs 3.5: a range is split into as many parts of at least one
+// round as the chip has compute units for, if that saves three rounds (12 heads x 1 query, us, whole and split:
+// 512 keys 7.4 and 9.0, 1024 10.0 and 9.2, 2048 15.2 and 9.3, 32768 174 and 23.6 in 21).  More than 64 parts
+// cost the merge more than they save (2 heads x 65536 keys: 64 parts 16.3, 128 parts 18.4).
+AttnPlan attn_plan_mx8(int32_t B, int32_t H, int32_t N, int32_t n_keys, size_t scratch) {
+  if (N > kMx8FewQueries) return attn_plan(B, H, N, n_keys, scratch);
+  constexpr int64_t kRound = 4, kMostParts = 64, kWorthRounds = 3;
+  const int64_t heads = int64_t(B) * H, tk = (n_keys + kAttnBlockK - 1) / kAttnBlockK;
+  const int64_t slots = std::min<int64_t>(kAttnMaxGroups, int64_t(scratch / attn_workspace_bytes(1)));
+  int64_t parts = std::max<int64_t>(1, std::min({slots / heads, tk / kRound, kMostParts}));
+  const int64_t longest = (tk + parts - 1) / parts;
+  parts = (tk + longest - 1) / longest;
+  if ((tk + kRound - 1) / kRound - (longest + kRound - 1) / kRound < kWorthRounds) parts = 1;
+  return parts > 1 ? balanced(parts * heads, heads) : AttnPlan{int32_t(heads), 0, int32_t(heads), 0, 1};
+}
+
 }  // namespace unstep

@@ -174,10 +174,13 @@ constexpr size_t kAttnMaxWorkspace = attn_workspace_bytes(kAttnMaxGroups);
 
 // The plan whose partials fit `scratch` bytes.
 AttnPlan attn_plan(int32_t B, int32_t H, int32_t N, int32_t n_keys, size_t scratch = kAttnMaxWorkspace);
+// The same for a quantised cache.
+AttnPlan attn_plan_mx8(int32_t B, int32_t H, int32_t N, int32_t n_keys, size_t scratch = kAttnMaxWorkspace);
 
 hipError_t launch_window_attn(const AttnArgs& a, hipStream_t stream);
-// The merge of a split launch's partials (nothing for a launch without them).
-hipError_t launch_attn_combine(const AttnArgs& a, hipStream_t stream);
+// The merge of a split launch's partials (nothing for a launch without them), in `slices` slices side by side
+// (0: by attn_merge_slices).
+hipError_t launch_attn_combine(const AttnArgs& a, hipStream_t stream, int32_t slices = 0);
 
 // Attention of quantised queries over a quantised cache: `a` as above (its q, k_cache and v_cache are not
 // read), scores in base-2 units (a.scale is ln 2, so offsets and sums merge as those of bf16 launches).
@@ -188,6 +191,9 @@ struct Mx8AttnArgs {
   const uint8_t *v8, *v_scale;
 };
 hipError_t launch_mx8_attn(const Mx8AttnArgs& a, hipStream_t stream);
+// Its kernel for chunks of at most kMx8FewQueries tokens (a.parts work-groups per (batch, head)).
+constexpr int kMx8FewQueries = 16;
+hipError_t launch_mx8_attn_few(const Mx8AttnArgs& a, hipStream_t stream);
 
 // The allocation-free entry point's scratch on the current device: a static device array of
 // kAttnMaxWorkspace bytes whose device address is looked up once per device and kept.

@@ -124,7 +124,7 @@ inline int plan_attn(const unstep_cache* c, int32_t newest, int32_t f0, int32_t 
   }
   a->seg_l0[UNSTEP_MAX_SEGMENTS] = INT32_MAX;
   a->scale = scale > 0.f ? scale : 1.0f / std::sqrt(float(UNSTEP_HEAD_DIM));
-  const AttnPlan plan = attn_plan(c->B, c->H, N, a->n_keys, workspace ? ws_bytes : 0);
+  const AttnPlan plan = (c->mx8() ? attn_plan_mx8 : attn_plan)(c->B, c->H, N, a->n_keys, workspace ? ws_bytes : 0);
   a->parts = 1;
   if (plan.workspace > 0) {
     a->groups = plan.groups;

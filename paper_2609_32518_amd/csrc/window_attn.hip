@@ -645,17 +645,22 @@ struct Merge {
   }
 };
 
+// Work-groups of `rows` rows that a query tile's merge takes: a chunk of fewer queries than a tile has fewer.
+__host__ __device__ __forceinline__ uint32_t combine_groups(int32_t N, int32_t rows) {
+  return uint32_t((N < kBlockQ ? N : kBlockQ) + rows - 1) / uint32_t(rows);
+}
+
 template <int kSlices>
 __global__ __launch_bounds__(256) void attn_combine_kernel(AttnArgs a) {
   constexpr int kRows = kSlices == 1 ? 2 : 1;             // rows per thread, kRowStep apart
   constexpr int kRowStep = 8 / kSlices;
   constexpr int kCombineRows = kRowStep * kRows;          // rows per work-group
-  constexpr int kGroupsPerTile = kBlockQ / kCombineRows;
+  const uint32_t groups_per_tile = combine_groups(a.N, kCombineRows);
   int32_t qtiles;
   const Schedule sc = make_schedule(a, &qtiles);
-  const int32_t t = int32_t(blockIdx.x / kGroupsPerTile);              // (b, h, query tile)
+  const int32_t t = int32_t(blockIdx.x / groups_per_tile);             // (b, h, query tile)
   const int32_t qt = t % qtiles;
-  const int32_t row_base = int32_t(blockIdx.x % kGroupsPerTile) * kCombineRows;
+  const int32_t row_base = int32_t(blockIdx.x % groups_per_tile) * kCombineRows;
   if (qt * kBlockQ + row_base >= a.N) return;
   const int32_t slice = int32_t(threadIdx.x >> 5) % kSlices;
   const int32_t r0 = row_base + int32_t(threadIdx.x >> 5) / kSlices;
@@ -734,7 +739,7 @@ template <int kSlices>
 void launch_combine(const AttnArgs& a, hipStream_t stream) {
   const int64_t qtiles = int64_t(a.B) * a.H * ((a.N + kBlockQ - 1) / kBlockQ);
   constexpr int kRows = 8 / kSlices * (kSlices == 1 ? 2 : 1);
-  hipLaunchKernelGGL(attn_combine_kernel<kSlices>, dim3(unsigned(qtiles * (kBlockQ / kRows))), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(attn_combine_kernel<kSlices>, dim3(unsigned(qtiles * combine_groups(a.N, kRows))), dim3(256), 0, stream, a);
 }
 
 }  // namespace
@@ -752,9 +757,10 @@ hipError_t launch_window_attn(const AttnArgs& a, hipStream_t stream) {
   return e == hipSuccess ? launch_attn_combine(a, stream) : e;
 }
 
-hipError_t launch_attn_combine(const AttnArgs& a, hipStream_t stream) {
+hipError_t launch_attn_combine(const AttnArgs& a, hipStream_t stream, int32_t slices) {
   if (a.part_o == nullptr) return hipSuccess;
-  switch (a.parts ? attn_merge_slices(a.B * a.H * ((a.N + kBlockQ - 1) / kBlockQ), a.parts) : 1) {
+  if (slices == 0) slices = a.parts ? attn_merge_slices(a.B * a.H * ((a.N + kBlockQ - 1) / kBlockQ), a.parts) : 1;
+  switch (slices) {
     case 1: launch_combine<1>(a, stream); break;
     case 2: launch_combine<2>(a, stream); break;
     case 4: launch_combine<4>(a, stream); break;
