@@ -309,21 +309,26 @@ __device__ __forceinline__ void step(Acc& a, Stage& st, Walk& w, const Queries& 
   barrier();
 }
 
-// Frees the rings and fills their first slots (K 0, K 1, V 0); K 2 and V 1 are on their way.
+// A walk's first loads, all at once: K 0 and V 0, K 1, and K 2 and V 1, which stay in st.
+struct Start {
+  Stage first, second;
+};
 template <bool kOneRun>
-__device__ __forceinline__ void walk_begin(Stage& st, Walk& w) {
+__device__ __forceinline__ void walk_load(Start& b, Stage& st, Walk& w) {
   if (!kOneRun) {
     cursor_at(w.seg, w.k_end, w.k_begin, w.kc);
     w.vc = w.kc;
   }
-  Stage second;
-  load_stage<kOneRun>(st, w, 0, 0);
-  load_stage<kOneRun>(second, w, min(1, w.n - 1), 0);
-  __syncthreads();
-  store_k(st, w, 0);
-  store_v(st, w, 0);
-  store_k(second, w, 1);
+  load_stage<kOneRun>(b.first, w, 0, 0);
+  load_stage<kOneRun>(b.second, w, min(1, w.n - 1), 0);
   load_stage<kOneRun>(st, w, min(2, w.n - 1), min(1, w.n - 1));
+}
+// Fills the rings' first slots, which every wave has left.
+__device__ __forceinline__ void walk_fill(const Start& b, const Walk& w) {
+  barrier();
+  store_k(b.first, w, 0);
+  store_v(b.first, w, 0);
+  store_k(b.second, w, 1);
 }
 
 template <int kMode, bool kOneRun, bool kIdle>
@@ -350,12 +355,15 @@ __device__ __forceinline__ void walk(Acc& a, Stage& st, Walk& w, const Queries& 
 // (rare, so it has one path, with the loader of any number of runs).
 template <bool kIdle>
 __device__ __forceinline__ void walk_again(Acc& a, Stage& st, Walk& w, const Queries& q, int group) {
-  walk_begin<false>(st, w);
+  Start b;
+  walk_load<false>(b, st, w);
+  walk_fill(b, w);
   walk<2, false, kIdle>(a, st, w, q, group);
   const float m = fmaxf(a.mx, __shfl_xor(a.mx, 32));
 #pragma unroll
   for (int i = 0; i < 16; ++i) a.negm[i] = -m;
-  walk_begin<false>(st, w);
+  walk_load<false>(b, st, w);
+  walk_fill(b, w);
   walk<1, false, kIdle>(a, st, w, q, group);
 }
 
@@ -417,11 +425,14 @@ __global__ __launch_bounds__(kThreads) void mx8_attn_kernel(Mx8AttnArgs m) {
     w.k_end = min(a.n_keys, sg.k1 * kBlockK);
     w.n = (w.k_end - w.k_begin + kBlockK - 1) / kBlockK;
     const bool one_run = w.k_end <= w.seg.l1;
+    // the first tiles' loads and the queries' are on their way together: a first touch of memory takes about
+    // 2 us, which a launch of few tiles would otherwise pay two or three times
     Stage st;
+    Start start;
     if (one_run)
-      walk_begin<true>(st, w);
+      walk_load<true>(start, st, w);
     else
-      walk_begin<false>(st, w);
+      walk_load<false>(start, st, w);
 
     const int32_t r = wave * 32 + col, qi = qt * kBlockQ + r;
     Queries q;
@@ -432,6 +443,7 @@ __global__ __launch_bounds__(kThreads) void mx8_attn_kernel(Mx8AttnArgs m) {
       q.f[1] = join(qp[4], qp[6]);
       q.scale = int(*reinterpret_cast<const uint32_t*>(m.q_scale + qrow * kMxBlocks) >> (8 * half));
     }
+    walk_fill(start, w);
     Acc acc;
     // a wave whose 32 queries all lie past the chunk's end runs the loads and barriers only
     const bool idle = qt * kBlockQ + wave * 32 >= N;
