@@ -109,12 +109,17 @@ SHAPES = [  # B, H, gh, gw, S, R, f0, C, W
     (1, 5, 3, 5, 1, 4, 9, 1, 3), (1, 2, 4, 8, 0, 30, 33, 1, 29), (2, 2, 3, 11, 0, 40, 45, 1, 38),
     (1, 3, 5, 13, 2, 7, 20, 1, 5), (1, 2, 7, 9, 0, 5, 4, 1, 4),
     (1, 2, 8, 16, 0, 12, 30, 2, 9), (1, 1, 16, 16, 0, 3, 2, 1, 2), (2, 5, 17, 23, 2, 8, 17, 2, 5),
-    (1, 24, 13, 30, 0, 9, 8, 1, 7), (1, 3, 30, 52, 3, 6, 9, 3, 3)]
+    (1, 24, 13, 30, 0, 9, 8, 1, 7), (1, 3, 30, 52, 3, 6, 9, 3, 3),
+    (1, 16, 4, 4, 0, 90, 89, 1, 89), (1, 16, 1, 17, 0, 90, 89, 1, 89),     # either side of the few-query kernel
+    (1, 130, 4, 5, 0, 80, 79, 1, 79),       # more query tiles than half the chip: one contiguous split of all of them
+    (2, 66, 4, 5, 2, 90, 200, 1, 85)]       # the same over two runs
 
 
 @pytest.mark.parametrize("shape", SHAPES)
 def test_every_element(shape):
     c = Case(*shape)
+    if shape[1] * shape[0] > 128:                              # the general kernel: work-groups that no tile divides
+        assert c.cache.workspace_bytes(*c.a) == 256 * 2 * 256 * 130 * 4
     want = c.expected()
     for split in (True, False):
         log(f"{shape} split={split}")
@@ -134,7 +139,7 @@ def test_scratch_of_any_size(shape):
         assert (ws[n:] == 255).all()
 
 
-@pytest.mark.parametrize("shape,step", [((1, 2, 8, 16, 0, 12, 30, 2, 9), 40.0), ((1, 3, 1, 1, 0, 900, 900, 1, 899), 60.0),
+@pytest.mark.parametrize("shape,step", [((1, 130, 4, 5, 0, 80, 79, 1, 79), 30.0), ((1, 2, 8, 16, 0, 12, 30, 2, 9), 40.0), ((1, 3, 1, 1, 0, 900, 900, 1, 899), 60.0),
                                         ((2, 1, 16, 17, 0, 8, 9, 2, 5), 25.0)])
 def test_scores_that_grow_along_the_keys(shape, step):
     """Later keys score hundreds of units above the first ones: sums and outputs stay finite and right."""

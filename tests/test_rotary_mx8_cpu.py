@@ -99,6 +99,21 @@ def test_append_refusals(kind, rc, kw):
         u.lib.unstep_cache_destroy(h)
 
 
+def test_size_refusals():
+    _, h = handle(True, H=33)
+    _, big = handle(True, H=31, gh=2048, gw=1024, S=0, R=3)     # a frame of 2^21 tokens x 31 heads is allowed
+    try:
+        strides = dict(ts=33 * 128, hs=128)
+        assert append(h, "mx8", wq=A[12], wk=A[13], **strides) == u.E_SHAPE            # more heads than a token's waves hold
+        assert append(h, "mx8", ts=2 ** 32 + 8, hs=128) == u.E_SHAPE
+        assert append(big, "mx8", C=3, ts=31 * 128, hs=128) == u.E_SHAPE               # 3 of them are not, in one chunk
+        assert u.lib.unstep_cache_advance(big, 0, 3) == u.OK
+        assert u.lib.unstep_kv_read_mx8(big, 0, 3, A[4], A[5], None) == u.E_SHAPE      # 3 x 2^21 x 31 rows
+    finally:
+        u.lib.unstep_cache_destroy(h)
+        u.lib.unstep_cache_destroy(big)
+
+
 def test_one_kind_of_cache_refuses_the_others_calls():
     _, hb = handle(False)
     _, hq = handle(True)
