@@ -79,13 +79,28 @@ AttnPlan attn_plan(int32_t B, int32_t H, int32_t N, int32_t n_keys, size_t scrat
   return plan_of(B, H, N, n_keys, int64_t(scratch / attn_workspace_bytes(1)));
 }
 
+namespace {
+// More than kMx8FewQueries queries: the bf16 kernel's split (measured within 3% of the best number of parts over
+// 14 shapes), and where there are more query tiles than compute units, the contiguous split over all of them
+// unless whole tiles fill their last round: 1.17 us per key tile of a whole one, 1.28 per unit of the split and
+// 17 for its partials (288 tiles x 141 key tiles 336 whole, 242 split).
+AttnPlan plan_many(int32_t B, int32_t H, int32_t N, int32_t n_keys, size_t scratch) {
+  const AttnPlan plan = attn_plan(B, H, N, n_keys, scratch);
+  const int64_t qtiles = plan.plain_groups, tk = (n_keys + kAttnBlockK - 1) / kAttnBlockK;
+  if (qtiles <= kAttnMaxGroups || plan.workspace > 0 || scratch < kAttnMaxWorkspace) return plan;
+  const double whole = double((qtiles + kAttnMaxGroups - 1) / kAttnMaxGroups) * double(tk) * 1.17;
+  const double split = double((qtiles * tk + kAttnMaxGroups - 1) / kAttnMaxGroups) * 1.28 + 17.0;
+  return split < whole ? balanced(kAttnMaxGroups, qtiles) : plan;
+}
+}  // namespace
+
 // Few queries: equal parts of a (batch, head)'s keys, one work-group each.  A work-group takes 256 keys (four
 // tiles) at a time, 1.33 us a round, and a merge costs 3.5: a range is split into as many parts of at least one
 // round as the chip has compute units for, if that saves three rounds (12 heads x 1 query, us, whole and split:
 // 512 keys 7.4 and 9.0, 1024 10.0 and 9.2, 2048 15.2 and 9.3, 32768 174 and 23.6 in 21).  More than 64 parts
 // cost the merge more than they save (2 heads x 65536 keys: 64 parts 16.3, 128 parts 18.4).
 AttnPlan attn_plan_mx8(int32_t B, int32_t H, int32_t N, int32_t n_keys, size_t scratch) {
-  if (N > kMx8FewQueries) return attn_plan(B, H, N, n_keys, scratch);
+  if (N > kMx8FewQueries) return plan_many(B, H, N, n_keys, scratch);
   constexpr int64_t kRound = 4, kMostParts = 64, kWorthRounds = 3;
   const int64_t heads = int64_t(B) * H, tk = (n_keys + kAttnBlockK - 1) / kAttnBlockK;
   const int64_t slots = std::min<int64_t>(kAttnMaxGroups, int64_t(scratch / attn_workspace_bytes(1)));

@@ -112,7 +112,8 @@ SHAPES = [  # B, H, gh, gw, S, R, f0, C, W
     (1, 24, 13, 30, 0, 9, 8, 1, 7), (1, 3, 30, 52, 3, 6, 9, 3, 3),
     (1, 16, 4, 4, 0, 90, 89, 1, 89), (1, 16, 1, 17, 0, 90, 89, 1, 89),     # either side of the few-query kernel
     (1, 130, 4, 5, 0, 80, 79, 1, 79),       # more query tiles than half the chip: one contiguous split of all of them
-    (2, 66, 4, 5, 2, 90, 200, 1, 85)]       # the same over two runs
+    (2, 66, 4, 5, 2, 90, 200, 1, 85),       # the same over two runs
+    (1, 300, 4, 5, 0, 70, 69, 1, 69)]       # more query tiles than compute units, split
 
 
 @pytest.mark.parametrize("shape", SHAPES)

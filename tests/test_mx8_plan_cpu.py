@@ -57,6 +57,42 @@ int main() {
     const AttnPlan a = attn_plan_mx8(1, 12, n, 18720), b = attn_plan(1, 12, n, 18720);
     CHECK(a.groups == b.groups && a.parts == b.parts && a.workspace == b.workspace);
   }
+  // more query tiles than compute units: contiguous ranges of units, every unit once, at most two partials each
+  int splits = 0;
+  for (int i = 0; i < 3000; ++i) {
+    const int H = 257 + rand() % 1200, keys = 1 + rand() % 20000;
+    const AttnPlan p = attn_plan_mx8(1, H, 17 + rand() % 240, keys, rand() % 4 ? kAttnMaxWorkspace : kAttnMaxWorkspace - 16);
+    if (p.workspace == 0) {
+      CHECK(p.groups == H);
+      continue;
+    }
+    ++splits;
+    CHECK(p.groups == kAttnMaxGroups && p.parts == 0 && p.workspace == kAttnMaxWorkspace);
+    Schedule sc;
+    sc.Tk = (keys + kAttnBlockK - 1) / kAttnBlockK;
+    sc.U = int64_t(H) * sc.Tk;
+    sc.G = p.groups;
+    int64_t next = sc.U;
+    for (int g = kAttnMaxGroups - 1; g >= 0; --g) {
+      int64_t hi = sc.start(g + 1);
+      const int64_t lo = sc.start(g);
+      CHECK(hi == next && lo < hi);
+      int partials[2] = {0, 0};
+      while (hi > lo) {
+        const Segment s = take_segment(sc, lo, hi);
+        CHECK(s.k0 < s.k1 && s.k1 <= sc.Tk && hi == s.t * sc.Tk + s.k0);
+        if (!s.full) {
+          CHECK(++partials[s.slot] == 1);
+          const int64_t ga = sc.owner(s.t * sc.Tk), gb = sc.owner(s.t * sc.Tk + sc.Tk - 1);
+          CHECK(ga <= g && g <= gb && ga < gb);
+          CHECK(s.slot == (g == ga ? (sc.start(ga) >= s.t * sc.Tk ? 0 : 1) : 0));   // where the merge looks for it
+        }
+      }
+      next = lo;
+    }
+    CHECK(next == 0);
+  }
+  CHECK(splits > 100);
   std::printf("ok\n");
 }
 """
