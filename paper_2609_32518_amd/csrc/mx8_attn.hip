@@ -269,7 +269,7 @@ __device__ __forceinline__ void v_phase(Acc& a, Stage& st, Walk& w, int32_t t) {
     float m = a.s[0][0];
 #pragma unroll
     for (int i = 0; i < 16; ++i) m = fmaxf(fmaxf(m, a.s[0][i]), a.s[1][i]);
-    m = fmaxf(m, __shfl_xor(m, 32));
+    m = fmaxf(fmaxf(m, __shfl_xor(m, 32)), -FLT_MAX);   // finite: scores of -infinity weigh nothing
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       a.negm[i] = -m;
@@ -359,7 +359,7 @@ __device__ __forceinline__ void walk_again(Acc& a, Stage& st, Walk& w, const Que
   walk_load<false>(b, st, w);
   walk_fill(b, w);
   walk<2, false, kIdle>(a, st, w, q, group);
-  const float m = fmaxf(a.mx, __shfl_xor(a.mx, 32));
+  const float m = fmaxf(fmaxf(a.mx, __shfl_xor(a.mx, 32)), -FLT_MAX);
 #pragma unroll
   for (int i = 0; i < 16; ++i) a.negm[i] = -m;
   walk_load<false>(b, st, w);

@@ -13,6 +13,8 @@
 // Running maximum, rescaled when it grows.  At the end the waves' sums meet in LDS, in one order.
 #include <hip/hip_runtime.h>
 
+#include <cfloat>
+
 #include "attn_schedule.hpp"
 #include "kernels.hpp"
 #include "mx8.hpp"
@@ -168,7 +170,7 @@ __global__ __launch_bounds__(kThreads) void mx8_attn_few_kernel(Mx8AttnArgs m) {
              SegTable{a.seg_l0[1], a.seg_l0[2], a.seg_l0[3], a.seg_row0[0], a.seg_row0[1], a.seg_row0[2], a.seg_row0[3]},
              min(begin + slice, k_end)};
   State st;
-  st.m = -INFINITY;
+  st.m = -FLT_MAX;                             // finite: scores of -infinity weigh nothing, also before any other
   st.l = 0.f;
 #pragma unroll
   for (int d = 0; d < 8; ++d) st.o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -205,7 +207,7 @@ __global__ __launch_bounds__(kThreads) void mx8_attn_few_kernel(Mx8AttnArgs m) {
   float top = part_m[0][qi];
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) top = fmaxf(top, part_m[w][qi]);
-  const float f = __builtin_amdgcn_exp2f(st.m - top);      // 0 for a wave without keys
+  const float f = __builtin_amdgcn_exp2f(st.m - top);
   float* const sums = reinterpret_cast<float*>(lds);
   if (qi < N) {
 #pragma unroll
@@ -225,7 +227,7 @@ __global__ __launch_bounds__(kThreads) void mx8_attn_few_kernel(Mx8AttnArgs m) {
       l += part_l[w][n] * __builtin_amdgcn_exp2f(part_m[w][n] - mm);
       o += *reinterpret_cast<const f32x4_t*>(sums + (w * kMaxQ + n) * kHeadDim + 4 * d4);
     }
-    o *= 1.f / l;
+    o *= a.parts == 1 || l > 0.f ? 1.f / l : 0.f;         // a part may hold nothing but scores of -infinity
     if (a.parts == 1) {
       bf16x4_t v;
 #pragma unroll

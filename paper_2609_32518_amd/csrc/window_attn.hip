@@ -631,7 +631,7 @@ constexpr int kCombineBatch = 4;                          // partials loaded tog
 struct Merge {
   float M, W;
   float4 acc;
-  // adds w (m, v), w = l 2^((m - M) c2), with l > 0 or an empty partial
+  // adds w (m, v), w = l 2^((m - M) c2)
   __device__ __forceinline__ void add(float m, float l, float4 v, float c2) {
     const float mn = fmaxf(M, m);
     const float s_old = __builtin_amdgcn_exp2f((M - mn) * c2);
@@ -698,8 +698,8 @@ __global__ __launch_bounds__(256) void attn_combine_kernel(AttnArgs a) {
     for (int i = 0; i < kCombineBatch; ++i) {
       if (g0 + i * kSlices > gb) break;
 #pragma unroll
-      for (int j = 0; j < kRows; ++j)                                  // an empty partial adds nothing
-        mg[j].add(ml[i][j].y > 0.f ? ml[i][j].x : -FLT_MAX, ml[i][j].y > 0.f ? ml[i][j].y : 0.f, v[i][j], c2);
+      for (int j = 0; j < kRows; ++j)                                  // an empty partial (sum 0) adds nothing, a NaN one NaN
+        mg[j].add(ml[i][j].y > 0.f ? ml[i][j].x : -FLT_MAX, ml[i][j].y, v[i][j], c2);
     }
   }
   if constexpr (kSlices > 1) {

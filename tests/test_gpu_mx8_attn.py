@@ -203,6 +203,37 @@ def test_large_scales_and_one_head_of_nan():
     assert (np.abs(got - keep(want[0])) <= 2.0 ** -7 * keep(want[2]) + 2.0 ** -17 * keep(want[2]) * (1 + want[3])).all()
 
 
+@pytest.mark.parametrize("shape,hidden", [((1, 2, 8, 16, 0, 12, 30, 2, 9), 700), ((1, 2, 8, 16, 0, 12, 30, 2, 9), 40), ((1, 3, 1, 1, 0, 900, 900, 1, 899), 300),
+                                          ((2, 1, 3, 3, 0, 9, 8, 1, 8), 40), ((1, 5, 1, 1, 0, 5000, 5200, 1, 4999), 2000)])
+@pytest.mark.parametrize("where", ["first", "last"])
+def test_scores_of_minus_infinity_weigh_nothing(shape, hidden, where):
+    """Products that overflow to -infinity for a run of keys: the others' attention, also where a tile, a wave's or
+    a work-group's whole share is such keys."""
+    c = Case(*shape)
+    q, k = mx8.values(*c.q), mx8.values(*c.k)
+    gone = c.rows[:hidden] if where == "first" else c.rows[-hidden:]
+    q[..., 0], k[..., 0] = 2.0 ** 66, 0.0
+    k[:, :, gone, 0] = -2.0 ** 66
+    c.q, c.k = mx8.quantise(q), mx8.quantise(k)
+    c.make()
+    c.rows = np.setdiff1d(c.rows, gone)
+    want = c.expected()
+    for split in (True, False):
+        c.check(*c.run(use_split=split), want)
+
+
+@pytest.mark.parametrize("shape", [(1, 2, 1, 1, 0, 5000, 5200, 1, 4999), (1, 2, 8, 16, 0, 12, 30, 2, 9)])
+@pytest.mark.parametrize("key", [0, 1000, -1])
+def test_a_nan_key_reaches_output_and_log_sum(shape, key):
+    """In one part of a split range as in the whole one."""
+    c = Case(*shape)
+    c.cache.k8.view(torch.uint8)[0, 1, int(c.rows[key]), 3] = 0x7F
+    for split in (True, False):
+        out, lse = c.run(use_split=split)
+        assert torch.isnan(out[:, :, 1]).all() and torch.isnan(lse[:, 1]).all()
+        assert torch.isfinite(out[:, :, 0]).all() and torch.isfinite(lse[:, 0]).all()
+
+
 def test_rows_past_two_gigabytes():
     """Offsets past 2^32 bytes: the last head of a cache whose rows lie beyond."""
     H, R, W = 34, 1024 * 1024, 2048
