@@ -23,6 +23,8 @@ What it defines, each in fp64 unless the paper fixes a precision:
                   attention windows (Sections 3.2-3.4, Appendix A.2 and A.3).
 * ``svd``      -- the rank-r truncation of the value and output weights and the
                   projection after attention (Section 3.5, Appendix A.4).
+* ``mx8``      -- the rotary options (layouts, part of the head, scaled tables) and the
+                  quantised cache: its number format, append and attention.
 * ``numerics`` -- the bf16 / binary32 rounding helpers the rest build on.
 
 Where the paper is silent, the reading taken is stated in the function that
