@@ -156,7 +156,9 @@ __device__ __forceinline__ void store_mx8(const F8& y, uint8_t* x8, uint8_t* sca
     d = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(d, y.v[4 * i + 2], y.v[4 * i + 3], s, true);
     w[i] = __builtin_bit_cast(uint32_t, d);
   }
-  __builtin_nontemporal_store(w, reinterpret_cast<u32x2_t*>(x8 + row * kHeadDim + p * 8));
+  // kept in the caches: what follows an append reads them (with a read-back 30.2 us instead of 33.5 for 4680 tokens x
+  // 12 heads, a step the same; the append alone 12.6 instead of 12.4, normalising 16.5 instead of 15.7)
+  *reinterpret_cast<u32x2_t*>(x8 + row * kHeadDim + p * 8) = w;
   uint32_t bytes = uint32_t(byte) << (8 * (p >> 2));
   bytes |= dpp<0x124>(bytes);                             // row_ror 4
   bytes |= dpp<0x128>(bytes);                             // row_ror 8
@@ -231,11 +233,11 @@ __global__ __launch_bounds__(kThreads) void rotary_append_kernel(RotaryAppendArg
 // ---- with the RMS normalisation: a token's head vectors on ceil(heads / 4) waves, one piece per lane as above.
 // x'_j = bf16(fp32(x_j r w_j)), r = 1 / sqrt(sum x^2 / channels + eps) in fp64 (each bf16 square is exact), summed
 // over a wave by exchanges and over the token's waves through LDS, in one order.
-// What bounds it is arithmetic beside the memory traffic: 4680 tokens x 12 heads take 15.8 us into the quantised
-// cache (67.7 MB; 12.5 without the normalisation, the rate of a copy) and 15.1 into the bf16 one (88.7 MB; 14.3).
-// Before: fp64 products per channel and a wave per token 21.4; binary32 pairs 17.5; one piece per lane,
-// divisions by multiplication and two Newton steps for the root 16.0; 64 registers, so that 8 waves fit a
-// SIMD, and the values stored before the statistic is known 15.8.
+// What bounds it is arithmetic beside the memory traffic: 4680 tokens x 12 heads take 16.5 us into the quantised
+// cache (67.7 MB; 12.6 without the normalisation, the rate of a copy) and 15.2 into the bf16 one (88.7 MB; 14.3).
+// Before, with stores past the caches: fp64 products per channel and a wave per token 21.4; binary32 pairs 17.5;
+// one piece per lane, divisions by multiplication and two Newton steps for the root 16.0; 64 registers, so that 8
+// waves fit a SIMD, and the values stored before the statistic is known 15.8.
 __device__ __forceinline__ double sum_sq(u32x4_t x) {
   double s = 0.0;
 #pragma unroll
