@@ -6,7 +6,7 @@
 
 #include <algorithm>
 #include <cmath>
-#include <new>
+#include <limits>
 
 #include "kernels.hpp"
 #include "plan.hpp"
@@ -44,16 +44,22 @@ int check_rotary(const unstep_rotary* r, const char* where) {
   return UNSTEP_OK;
 }
 
-// Angle per position of every pair, and the tables' amplitude.
+// Angle per position of every pair, and the tables' amplitude.  w_k = theta^(-2k/d) is a chain of extended
+// products (64 fraction bits; the 63rd is within 2^-56 before its rounding to binary64): one power an axis, where one
+// a pair took 1.6 of a small call's 5.9 us.
 void frequencies(const unstep_rotary& r, unstep::RotaryTableArgs* a) {
+  static_assert(std::numeric_limits<long double>::digits >= 64, "the chain needs guard bits");
   const int32_t dims[3] = {r.dim_t, r.dim_h, r.dim_w};
   double* w = a->freq;
   for (int axis = 0; axis < 3; ++axis) {
     const int32_t d = dims[axis];
-    double theta = r.theta;
-    if (axis == 0 && r.scaling == UNSTEP_ROTARY_BASE && d > 2) theta *= std::pow(r.factor, double(d) / (d - 2.0));
-    for (int32_t k = 0; k < d / 2; ++k) {
-      double f = 1.0 / std::pow(theta, (2.0 * k) / double(d));
+    if (d == 0) continue;
+    long double theta = r.theta;
+    if (axis == 0 && r.scaling == UNSTEP_ROTARY_BASE && d > 2) theta *= std::pow((long double)r.factor, (long double)d / (d - 2));
+    const long double ratio = std::pow(theta, -2.0L / d);
+    long double x = 1.0L;
+    for (int32_t k = 0; k < d / 2; ++k, x *= ratio) {
+      double f = double(x);
       if (axis == 0 && r.scaling == UNSTEP_ROTARY_LINEAR) f /= r.factor;
       if (axis == 0 && r.scaling == UNSTEP_ROTARY_PARTS) {
         const double turns = r.trained_frames * f / (2.0 * M_PI);
