@@ -67,10 +67,14 @@ class CacheMX8:
     _workspace_bytes = Cache._workspace_bytes
 
     def workspace(self, start_frame: int, n_frames: int, window_frames: int) -> Optional[torch.Tensor]:
-        """Device scratch for split-key attention, grown on demand and kept."""
+        """Device scratch for split-key attention, grown on demand and kept; while a graph is captured a new one, which
+        the graph's memory pool holds: the kept one may be replaced, or in use elsewhere, when the graph is replayed.
+        Calls that may overlap otherwise (two streams) need a workspace argument each."""
         need = self.workspace_bytes(start_frame, n_frames, window_frames)
         if need == 0:
             return None
+        if self.device.type == "cuda" and torch.cuda.is_current_stream_capturing():
+            return torch.empty(need, dtype=torch.uint8, device=self.device)
         if self._ws is None or self._ws.numel() < need:
             self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
         return self._ws

@@ -5,6 +5,7 @@
 #include "common.hpp"
 
 #include <c10/hip/HIPFunctions.h>
+#include <c10/hip/HIPGraphsC10Utils.h>
 
 #include <cstring>
 
@@ -96,6 +97,12 @@ struct Queries {
     return scale != nullptr;
   }
 };
+
+// Whether a call would take the kept scratch into a captured graph, which needs one of its own: the Python path.
+bool captures_scratch(PyObject* given, PyObject* use_split) {
+  if (given != Py_None || use_split == Py_False) return false;
+  return current_stream() && c10::hip::currentStreamCaptureStatusMayInitCtx() != c10::hip::CaptureStatus::None;
+}
 
 // (a, b) as a tuple, made before the library's call.
 Ref pair(PyObject* given_a, const at::Tensor& a, PyObject* given_b, const at::Tensor& b) {
@@ -219,7 +226,7 @@ PyObject* f_window_attn_mx8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     size_t bytes;
     at::Tensor made, hold;
     Queries q{};
-    if (a[4] == Py_None || a[5] == Py_None || !q.get(*c, N, a[4], a[5]) || !lse_of(*c, N, a[7], &lse) ||
+    if (captures_scratch(a[8], a[9]) || a[4] == Py_None || a[5] == Py_None || !q.get(*c, N, a[4], a[5]) || !lse_of(*c, N, a[7], &lse) ||
         !workspace_of(*c, f0, C, W, a[8], a[9], a[10], false, &hold, &ws, &bytes))
       return none();
     const at::Tensor* out = chunk_out(*c, N, a[6], &made);
@@ -246,7 +253,7 @@ PyObject* f_step_mx8(PyObject*, PyObject* const* a, Py_ssize_t n) {
     size_t bytes;
     at::Tensor made, hold;
     Queries q{};
-    if (!c || !chunk_of(*c, a + 1, false, -1, &k) || !to_i32(a[8], &W) || !layout_of(a[9], &layout) ||
+    if (!c || captures_scratch(a[18], a[19]) || !chunk_of(*c, a + 1, false, -1, &k) || !to_i32(a[8], &W) || !layout_of(a[9], &layout) ||
         !norm_of(*c, true, a[10], a[11], a[12], &wq, &wk, &eps) || !to_f64(a[13], &scale) || !lse_of(*c, k.N, a[17], &lse) ||
         !workspace_of(*c, k.f0, k.C, W, a[18], a[19], a[20], false, &hold, &ws, &bytes) || !q.get(*c, k.N, a[14], a[15]))
       return none();

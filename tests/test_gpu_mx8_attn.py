@@ -324,6 +324,47 @@ def test_step_replayed_from_a_graph():
         assert torch.equal(out.view(torch.int16), eager.view(torch.int16))
 
 
+@pytest.mark.parametrize("whole_step", [False, True])
+def test_captures_have_scratch_of_their_own(whole_step):
+    """Two graphs of one cache, captured without a workspace argument, replayed at once on two streams and after the
+    kept scratch has grown and its old memory has gone to another tensor."""
+    B, H, gh, gw, S, R, f0, C, W = 1, 4, 1, 1, 0, 5000, 4999, 1, 4000
+    c = Case(B, H, gh, gw, S, R, f0, C, W)
+    cos, sin = u.unstep_rotary_tables(f0, C, gh, gw, dims=(128, 0, 0))
+    qkv = [torch.randn(B, 1, H, 128, device="cuda", generator=torch.Generator(device="cuda").manual_seed(i)).bfloat16() for i in range(3)]
+
+    def call(window):
+        if whole_step:
+            return c.cache.unstep_step_mx8(f0, C, window, *qkv, cos, sin)
+        return c.cache.unstep_window_attn_mx8(f0, C, window, c.q8, c.qs)
+
+    want = {w: call(w).clone() for w in (3000, W)}
+    kept = c.cache._ws
+    graphs, outs = {}, {}
+    for w in want:
+        graphs[w] = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graphs[w]):
+            outs[w] = call(w)
+    assert c.cache._ws is kept
+    c.cache._ws = None                                         # as when a larger one replaces it
+    size = kept.numel()
+    del kept
+    other = torch.full((size,), 77, dtype=torch.uint8, device="cuda")
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for o in outs.values():
+            o.zero_()
+        torch.cuda.synchronize()
+        for s, w in zip(streams, want):
+            with torch.cuda.stream(s):
+                graphs[w].replay()
+        torch.cuda.synchronize()
+        assert (other == 77).all()
+        for w in want:
+            assert torch.equal(outs[w].view(torch.int16), want[w].view(torch.int16))
+
+
 def test_streams_and_kept_scratch():
     """A step on a named stream while the program goes on: the same result, and memory that the wrappers
     allocated is not handed out before that stream has used it."""
