@@ -125,17 +125,20 @@ __device__ __forceinline__ u32x4_t to_bf16(const F8& y) {
   return o;
 }
 
-// The scale byte of the block (4 lanes) that this lane's 8 values belong to.  Magnitudes compare as
-// integers; a value that is not finite, which does not count, sends the lane through its values again.
+// The scale byte of the block (4 lanes) that this lane's 8 values belong to.  A value that is not finite does not
+// count: a maximum leaves NaN out by itself, and one that is infinite (or nothing but NaN) sends the lane through
+// its values again.
 __device__ __forceinline__ int32_t block_byte(const F8& y) {
-  uint32_t m[8], top = 0;
+  float most = __builtin_fabsf(y.v[0]);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m[i] = __float_as_uint(y.v[i]) & 0x7fffffffu;
-#pragma unroll
-  for (int i = 0; i < 8; i += 2) top = max(max(m[i], m[i + 1]), top);
+  for (int i = 1; i < 8; ++i) most = __builtin_fmaxf(most, __builtin_fabsf(y.v[i]));
+  uint32_t top = __float_as_uint(most);
   if (__builtin_expect(top >= 0x7f800000u, 0)) {
     top = 0;
-    for (int i = 0; i < 8; ++i) top = m[i] < 0x7f800000u ? max(top, m[i]) : top;
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t m = __float_as_uint(y.v[i]) & 0x7fffffffu;
+      top = m < 0x7f800000u ? max(top, m) : top;
+    }
   }
   top = max(top, dpp<0xb1>(top));                         // quad_perm 1,0,3,2
   top = max(top, dpp<0x4e>(top));                         // quad_perm 2,3,0,1
@@ -157,7 +160,7 @@ __device__ __forceinline__ void store_mx8(const F8& y, uint8_t* x8, uint8_t* sca
     w[i] = __builtin_bit_cast(uint32_t, d);
   }
   // kept in the caches: what follows an append reads them (with a read-back 30.2 us instead of 33.5 for 4680 tokens x
-  // 12 heads, a step the same; the append alone 12.6 instead of 12.4, normalising 16.5 instead of 15.7)
+  // 12 heads, a step the same; the append alone 0.2 to 0.9 more)
   *reinterpret_cast<u32x2_t*>(x8 + row * kHeadDim + p * 8) = w;
   uint32_t bytes = uint32_t(byte) << (8 * (p >> 2));
   bytes |= dpp<0x124>(bytes);                             // row_ror 4
@@ -233,11 +236,12 @@ __global__ __launch_bounds__(kThreads) void rotary_append_kernel(RotaryAppendArg
 // ---- with the RMS normalisation: a token's head vectors on ceil(heads / 4) waves, one piece per lane as above.
 // x'_j = bf16(fp32(x_j r w_j)), r = 1 / sqrt(sum x^2 / channels + eps) in fp64 (each bf16 square is exact), summed
 // over a wave by exchanges and over the token's waves through LDS, in one order.
-// What bounds it is arithmetic beside the memory traffic: 4680 tokens x 12 heads take 16.5 us into the quantised
-// cache (67.7 MB; 12.6 without the normalisation, the rate of a copy) and 15.2 into the bf16 one (88.7 MB; 14.3).
-// Before, with stores past the caches: fp64 products per channel and a wave per token 21.4; binary32 pairs 17.5;
-// one piece per lane, divisions by multiplication and two Newton steps for the root 16.0; 64 registers, so that 8
-// waves fit a SIMD, and the values stored before the statistic is known 15.8.
+// What bounds it is memory and, between a token's loads and its stores, the statistic: 4680 tokens x 12 heads take
+// 15.8 us into the quantised cache (67.7 MB; 12.4 without the normalisation, the rate of a copy) and 14.9 into the bf16
+// one (88.7 MB; 14.3).  Before: fp64 products per channel and a wave per token 21.4; binary32 pairs 17.5; one piece per
+// lane, divisions by multiplication and two Newton steps for the root 16.0; 64 registers, so that 8 waves fit a SIMD,
+// and the values stored before the statistic is known 15.8; with stores that stay in the caches 16.5; two operations
+// a product instead of four and no branches around the loads 15.8.
 __device__ __forceinline__ double sum_sq(u32x4_t x) {
   double s = 0.0;
 #pragma unroll
@@ -295,8 +299,8 @@ __device__ __forceinline__ double wave_sums(double k, double q) {
 }
 
 // bf16(fp32(x r w)) for the 8 channels of a piece.  x w is exact in binary32 (8 and 8 bits); its product with
-// hi + lo, formed as p + (its error + x w lo), is within 2^-47 of the exact one before its only rounding to
-// binary32, as the fp64 product is within 2^-52: four binary32 operations instead of five conversions and
+// hi + lo, formed as fma(x w, hi, x w lo), is within 2^-47 of the exact one before its only rounding to
+// binary32, as the fp64 product is within 2^-52: two binary32 operations instead of five conversions and
 // products in fp64, which the pass's time went into.  The binary32 value is kept opaque, or the two roundings
 // would be folded into one.
 __device__ __forceinline__ u32x4_t normalise8(u32x4_t x, u32x4_t w, const Rms& m) {
@@ -307,8 +311,7 @@ __device__ __forceinline__ u32x4_t normalise8(u32x4_t x, u32x4_t w, const Rms& m
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float t = xs.v[i] * ws.v[i];
-      const float p = t * m.hi;
-      v.v[i] = p + __builtin_fmaf(t, m.lo, __builtin_fmaf(t, m.hi, -p));
+      v.v[i] = __builtin_fmaf(t, m.hi, t * m.lo);
     }
   } else {
 #pragma unroll
@@ -322,39 +325,36 @@ __device__ __forceinline__ u32x4_t normalise8(u32x4_t x, u32x4_t w, const Rms& m
 constexpr int kNormMaxWaves = kNormMaxHeads * kPieces / 64;   // of a token, and of a work-group
 static_assert(kNormMaxWaves == 8, "");
 
+// waves: of a token; tokens: of a work-group.  Lanes past the last head or token load and compute what the last one's
+// do, and neither count nor store.
 template <bool kWithQ, bool kHalf, bool kMx8>
-__global__ __launch_bounds__(kNormMaxWaves * 64, 8) void rotary_norm_append_kernel(RotaryAppendArgs r, int32_t waves) {
+__global__ __launch_bounds__(kNormMaxWaves * 64, 8) void rotary_norm_append_kernel(RotaryAppendArgs r, uint32_t waves,
+                                                                                   uint32_t tokens, FastDiv by_waves) {
   const RopeAppendArgs& a = r.a;
   __shared__ double sums[kNormMaxWaves][2];
-  const int32_t N = a.C * a.T;
+  const uint32_t last = uint32_t(a.C) * uint32_t(a.T) - 1;
   const int lane = threadIdx.x & 63;
-  const int32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int32_t tok = wave / waves, part = wave - tok * waves;               // of the work-group; wave of the token
-  const int32_t n = blockIdx.x * (int32_t(blockDim.x >> 6) / waves) + tok;
-  const int32_t b = blockIdx.y;
-  const int32_t h = 4 * part + (lane >> 4), p = lane % kPieces;
-  const bool here = n < N && h < a.H;                                        // the same for a head vector's 16 lanes
-  u32x4_t kx = {}, vx = {}, qx = {}, wk = {}, wq = {};
-  Turn<kHalf> t{};
-  if (here) {
-    const int64_t src = source(a, b, n, h, p);
-    kx = *reinterpret_cast<const u32x4_t*>(a.k + src);
-    if (kWithQ) qx = *reinterpret_cast<const u32x4_t*>(a.q + src);
-    t = load_turn<kHalf>(r, n, p);
-    vx = *reinterpret_cast<const u32x4_t*>(a.v + src);
-    wk = *reinterpret_cast<const u32x4_t*>(a.wk + h * kHeadDim + p * 8);
-    if (kWithQ) wq = *reinterpret_cast<const u32x4_t*>(a.wq + h * kHeadDim + p * 8);
-  }
-  const double s = wave_sums(sum_sq(kx), kWithQ ? sum_sq(qx) : 0.0);
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t tok = divide(wave, by_waves), part = wave - tok * waves;    // of the work-group; wave of the token
+  const uint32_t n0 = blockIdx.x * tokens + tok, n = min(n0, last);
+  const int32_t b = blockIdx.y, h0 = int32_t(4 * part) + (lane >> 4), h = min(h0, a.H - 1), p = lane % kPieces;
+  const bool here = n0 == n && h0 == h;                                      // the same for a head vector's 16 lanes
+  const int64_t src = source(a, b, n, h, p);
+  const u32x4_t kx = *reinterpret_cast<const u32x4_t*>(a.k + src);
+  u32x4_t qx = {}, wq = {};
+  if (kWithQ) qx = *reinterpret_cast<const u32x4_t*>(a.q + src);
+  const Turn<kHalf> t = load_turn<kHalf>(r, n, p);
+  const u32x4_t vx = *reinterpret_cast<const u32x4_t*>(a.v + src);
+  const u32x4_t wk = *reinterpret_cast<const u32x4_t*>(a.wk + h * kHeadDim + p * 8);
+  if (kWithQ) wq = *reinterpret_cast<const u32x4_t*>(a.wq + h * kHeadDim + p * 8);
+  const double sk = sum_sq(kx), sq = kWithQ ? sum_sq(qx) : 0.0;
+  const double s = wave_sums(here ? sk : 0.0, here ? sq : 0.0);
   if ((lane & 31) == 0) sums[wave][lane >> 5] = s;
-  Place at{};
-  if (here) {                                             // the values need no statistic
-    at = place(r, b, n, h);
-    put_value<kMx8>(r, vx, at, p);
-  }
+  const Place at = place(r, b, n, h);
+  if (here) put_value<kMx8>(r, vx, at, p);                // the values need no statistic
   __syncthreads();
   double ss = 0.0;
-  for (int32_t i = 0; i < waves; ++i) ss += sums[tok * waves + i][lane >> 5];
+  for (uint32_t i = 0; i < waves; ++i) ss += sums[tok * waves + i][lane >> 5];
   const double rr = inverse_root(ss * r.inv_channels + a.eps);
   const Rms rk = rms_of(lane_value(rr, 0)), rq = rms_of(lane_value(rr, 32));
   if (!here) return;
@@ -366,10 +366,10 @@ template <bool kWithQ, bool kHalf, bool kMx8>
 void launch(const RotaryAppendArgs& r, hipStream_t stream) {
   const RopeAppendArgs& a = r.a;
   if (a.wk) {
-    const int32_t waves = (a.H + 3) / 4, tokens = waves < 4 ? 4 / waves : 1;  // of a token; tokens of a work-group
-    const dim3 grid(unsigned((a.C * a.T + tokens - 1) / tokens), unsigned(a.B));
-    hipLaunchKernelGGL((rotary_norm_append_kernel<kWithQ, kHalf, kMx8>), grid, dim3(unsigned(waves * tokens * 64)), 0, stream, r,
-                       waves);
+    const uint32_t waves = uint32_t(a.H + 3) / 4, tokens = waves < 4 ? 4 / waves : 1;  // of a token; tokens of a work-group
+    const dim3 grid((uint32_t(a.C * a.T) + tokens - 1) / tokens, unsigned(a.B));
+    hipLaunchKernelGGL((rotary_norm_append_kernel<kWithQ, kHalf, kMx8>), grid, dim3(waves * tokens * 64), 0, stream, r, waves,
+                       tokens, fast_div(waves));
     return;
   }
   const int64_t units = int64_t(a.C) * a.T * a.H * kPieces;
