@@ -175,6 +175,9 @@ constexpr size_t kAttnMaxWorkspace = attn_workspace_bytes(kAttnMaxGroups);
 // The plan whose partials fit `scratch` bytes.
 AttnPlan attn_plan(int32_t B, int32_t H, int32_t N, int32_t n_keys, size_t scratch = kAttnMaxWorkspace);
 // The same for a quantised cache.
+constexpr int kMx8FewQueries = 16;
+// Whether a launch takes the kernel of kMx8FewQueries queries per work-group.
+bool mx8_few(int32_t B, int32_t H, int32_t N, int32_t n_keys);
 AttnPlan attn_plan_mx8(int32_t B, int32_t H, int32_t N, int32_t n_keys, size_t scratch = kAttnMaxWorkspace);
 
 hipError_t launch_window_attn(const AttnArgs& a, hipStream_t stream);
@@ -191,8 +194,7 @@ struct Mx8AttnArgs {
   const uint8_t *v8, *v_scale;
 };
 hipError_t launch_mx8_attn(const Mx8AttnArgs& a, hipStream_t stream);
-// Its kernel for chunks of at most kMx8FewQueries tokens (a.parts work-groups per (batch, head)).
-constexpr int kMx8FewQueries = 16;
+// Its kernel of kMx8FewQueries queries per work-group (a.parts work-groups where that is all of a (batch, head)'s).
 hipError_t launch_mx8_attn_few(const Mx8AttnArgs& a, hipStream_t stream);
 
 // The allocation-free entry point's scratch on the current device: a static device array of

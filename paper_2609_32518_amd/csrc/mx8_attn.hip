@@ -506,7 +506,7 @@ __global__ __launch_bounds__(kThreads) void mx8_attn_kernel(Mx8AttnArgs m) {
 }  // namespace
 
 hipError_t launch_mx8_attn(const Mx8AttnArgs& m, hipStream_t stream) {
-  if (m.a.N <= kMx8FewQueries) {
+  if (mx8_few(m.a.B, m.a.H, m.a.N, m.a.n_keys)) {
     const hipError_t e = launch_mx8_attn_few(m, stream);
     // few rows leave the chip to the slices: as many as leave each one batch of partials, loaded together
     const int32_t p = m.a.parts;

@@ -1,6 +1,6 @@
-// Attention of up to 16 quantised queries per (batch, head) over the retained rows of a quantised cache: a
-// single-token stream's call.  Bound by memory: every retained row is read once (264 bytes of K and V), and
-// 16 queries cost the same as one.
+// Attention of quantised queries, 16 per work-group, over the retained rows of a quantised cache: the call of a
+// single-token stream, and of small chunks.  Bound by memory: 16 queries read every retained row once (264
+// bytes of K and V) and cost the same as one; a short range by its chain of loads, 1.5 us per 256 keys.
 //
 // Work-group: 8 waves, each walking a slice of its own of the work-group's key range, 32 keys at a time, with
 // the next 32 keys' rows on their way to registers.  No wave waits for another before the end.
@@ -29,6 +29,7 @@ constexpr int kThreads = kWaves * 64;
 constexpr int kTile = 32;                      // keys per step of a wave
 constexpr int kAhead = 1;                      // steps whose rows are on their way (2: 2-5% slower)
 constexpr int kRow8 = kHeadDim, kRow16 = kHeadDim * 2;
+constexpr int kXcds = 8;
 constexpr int kMaxQ = kMx8FewQueries;
 static_assert(kMaxQ == 16, "one MFMA column per query");
 
@@ -160,9 +161,13 @@ __global__ __launch_bounds__(kThreads) void mx8_attn_few_kernel(Mx8AttnArgs m) {
   const AttnArgs& a = m.a;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int32_t N = a.N, H = a.H, grp = blockIdx.x;
+  const int32_t N = a.N, H = a.H, G = gridDim.x, tiles = (N + kMaxQ - 1) / kMaxQ;   // several only where a.parts is 1
+  // as in the general kernel: an XCD's work-groups are consecutive, so that a head's query tiles share its L2
+  const int32_t xcd = blockIdx.x % kXcds;
+  const int32_t grp = xcd * (G / kXcds) + min(xcd, G % kXcds) + blockIdx.x / kXcds;
   const Segment sg = part_segment((a.n_keys + kAttnBlockK - 1) / kAttnBlockK, a.parts, grp);
-  const int32_t bh = int32_t(sg.t), h = bh % H, b = bh / H;
+  const int32_t bh = int32_t(sg.t) / tiles, q0 = (int32_t(sg.t) - bh * tiles) * kMaxQ, h = bh % H, b = bh / H;
+  const int32_t here = min(N - q0, kMaxQ);                 // queries of this work-group
   const int64_t row0 = int64_t(bh) * a.slots;
   const int32_t k_begin = sg.k0 * kAttnBlockK, k_end = min(a.n_keys, sg.k1 * kAttnBlockK);
   const int32_t slice = ((k_end - k_begin + kWaves * kTile - 1) / (kWaves * kTile)) * kTile;
@@ -181,7 +186,7 @@ __global__ __launch_bounds__(kThreads) void mx8_attn_few_kernel(Mx8AttnArgs m) {
     for (int i = 0; i < kAhead; ++i) load(r[i], src, begin + i * kTile);
     u32x4_t q[4];
     {
-      const int64_t qrow = (int64_t(b) * N + min(lane & 15, N - 1)) * H + h;
+      const int64_t qrow = (int64_t(b) * N + min(q0 + (lane & 15), N - 1)) * H + h;
       const u32x4_t* qp = reinterpret_cast<const u32x4_t*>(m.q8 + qrow * kRow8 + 32 * g);
       const float sc = mx8_scale(m.q_scale[qrow * kMxBlocks + g]);
 #pragma unroll
@@ -210,14 +215,14 @@ __global__ __launch_bounds__(kThreads) void mx8_attn_few_kernel(Mx8AttnArgs m) {
   for (int w = 1; w < kWaves; ++w) top = fmaxf(top, part_m[w][qi]);
   const float f = __builtin_amdgcn_exp2f(st.m - top);
   float* const sums = reinterpret_cast<float*>(lds);
-  if (qi < N) {
+  if (qi < here) {
 #pragma unroll
     for (int d = 0; d < 8; ++d)
       *reinterpret_cast<f32x4_t*>(sums + (wave * kMaxQ + qi) * kHeadDim + 16 * d + 4 * g) = st.o[d] * f;
   }
   __syncthreads();
   // a thread finishes four dimensions of a query
-  for (int i = tid; i < N * (kHeadDim / 4); i += kThreads) {
+  for (int i = tid; i < here * (kHeadDim / 4); i += kThreads) {
     const int n = i / (kHeadDim / 4), d4 = i % (kHeadDim / 4);
     float mm = part_m[0][n], l = 0.f;
 #pragma unroll
@@ -233,8 +238,8 @@ __global__ __launch_bounds__(kThreads) void mx8_attn_few_kernel(Mx8AttnArgs m) {
       bf16x4_t v;
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = (__bf16)o[e];
-      *reinterpret_cast<bf16x4_t*>(a.out + ((int64_t(b) * N + n) * H + h) * kHeadDim + 4 * d4) = v;
-      if (a.lse && d4 == 0) a.lse[(int64_t(b) * H + h) * N + n] = mm * a.scale + logf(l);
+      *reinterpret_cast<bf16x4_t*>(a.out + ((int64_t(b) * N + q0 + n) * H + h) * kHeadDim + 4 * d4) = v;
+      if (a.lse && d4 == 0) a.lse[(int64_t(b) * H + h) * N + q0 + n] = mm * a.scale + logf(l);
     } else {
       const int64_t prow = int64_t(grp) * 2 * kAttnBlockQ + n;
       *reinterpret_cast<f32x4_t*>(a.part_o + prow * kHeadDim + 4 * d4) = o;

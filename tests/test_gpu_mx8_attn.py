@@ -127,6 +127,49 @@ def test_every_element(shape):
         c.check(*c.run(use_split=split), want)
 
 
+# Small chunks in groups of 16 queries: batch, odd sizes, sinks and a wrapped ring, a last group of one, a range of one
+# wave, and the first sizes past those (the general kernel)
+SMALL = [(3, 3, 1, 18, 0, 23, 22, 1, 22), (2, 5, 3, 7, 2, 9, 30, 1, 8), (1, 2, 17, 23, 1, 4, 9, 1, 3), (1, 24, 1, 33, 0, 6, 5, 2, 4),
+         (1, 15, 7, 37, 0, 3, 2, 1, 0), (2, 1, 30, 52, 0, 2, 1, 1, 0), (1, 12, 1, 17, 0, 30, 29, 1, 29), (1, 7, 17, 17, 1, 5, 14, 2, 3),
+         (1, 2, 16, 20, 0, 12, 30, 2, 9)]
+
+
+@pytest.mark.parametrize("shape", SMALL)
+def test_small_chunks(shape):
+    c = Case(*shape)
+    want = c.expected()
+    guard = torch.full((c.q8.shape[0] + 1,) + tuple(c.q8.shape[1:]), 3.0, device="cuda", dtype=torch.bfloat16)
+    for split in (True, False):
+        c.check(*c.run(use_split=split, out=guard[:-1]), want)
+        assert (guard[-1] == 3.0).all()
+
+
+@pytest.mark.parametrize("shape", [(1, 2, 8, 16, 0, 5, 4, 1, 4), (1, 2, 16, 20, 0, 12, 30, 2, 9)])
+def test_small_chunks_whose_scores_grow_or_vanish(shape):
+    """Both kernels: scores that grow by hundreds, then a run of keys whose scores are -infinity, then a NaN key."""
+    c = Case(*shape, q_scale=1.0)
+    n = len(c.rows)
+    q, k = mx8.values(*c.q), mx8.values(*c.k)
+    q[..., 0], k[..., 0] = 8.0, 0.0
+    k[:, :, c.rows, 0] = np.linspace(-40, 40, n)
+    c.q, c.k = mx8.quantise(q), mx8.quantise(k)
+    c.make()
+    for split in (True, False):
+        c.check(*c.run(use_split=split), E=c.cut())
+    c = Case(*shape)
+    q, k = mx8.values(*c.q), mx8.values(*c.k)
+    q[..., 0], k[..., 0] = 2.0 ** 66, 0.0
+    k[:, :, c.rows[:n // 2], 0] = -2.0 ** 66
+    c.q, c.k = mx8.quantise(q), mx8.quantise(k)
+    c.make()
+    every, c.rows = c.rows, c.rows[n // 2:]
+    c.check(*c.run(), c.expected())
+    c.cache.k8.view(torch.uint8)[0, 1, int(every[-1]), 100] = 0x7F
+    out, lse = c.run()
+    assert torch.isnan(out[:, :, 1]).all() and torch.isnan(lse[:, 1]).all()
+    assert torch.isfinite(out[:, :, 0]).all() and torch.isfinite(lse[:, 0]).all()
+
+
 @pytest.mark.parametrize("shape", [SHAPES[4], SHAPES[12], SHAPES[13]])
 def test_scratch_of_any_size(shape):
     """No scratch, too little, a part of it: fewer parts, the same result within the bound."""

@@ -110,3 +110,47 @@ def test_plan_and_divisors(tmp_path):
     assert r.returncode == 0, r.stderr[-3000:]
     r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr
+
+
+SMALL = r"""
+#include <cstdio>
+#include <cstdlib>
+#include "kernels.hpp"
+#include "seg_table.hpp"
+using namespace unstep;
+#define CHECK(x) do { if (!(x)) { std::printf("line %d: %s\n", __LINE__, #x); return 1; } } while (0)
+int main() {
+  srand(2);
+  int small = 0;
+  for (int i = 0; i < 50000; ++i) {
+    const int B = 1 + rand() % 3, H = 1 + rand() % 60, N = 17 + rand() % (1 << (3 + rand() % 10));
+    const int keys = 1 + rand() % (1 << (4 + rand() % 13));
+    if (!mx8_few(B, H, N, keys)) continue;
+    ++small;
+    const int tiles = (N + kMx8FewQueries - 1) / kMx8FewQueries;
+    for (size_t scratch : {size_t(0), size_t(kAttnMaxWorkspace)}) {
+      const AttnPlan p = attn_plan_mx8(B, H, N, keys, scratch);
+      CHECK(p.workspace == 0 && p.parts == 1 && p.groups == B * H * tiles && p.plain_groups == p.groups && p.groups <= kAttnMaxGroups);
+    }
+  }
+  CHECK(small > 1000);
+  CHECK(mx8_few(1, 1, 1, 1) && mx8_few(4, 400, 16, 1 << 20));          // up to 16 queries always
+  CHECK(mx8_few(1, 12, 27, 432) && mx8_few(1, 8, 512, 2048));
+  CHECK(!mx8_few(1, 12, 17, 18720) && !mx8_few(1, 12, 4680, 18720) && !mx8_few(1, 60, 32, 19200) && !mx8_few(1, 257, 17, 64));
+  std::printf("ok\n");
+}
+"""
+
+
+def test_small_chunks(tmp_path):
+    gxx = shutil.which("g++")
+    if gxx is None or not os.path.exists(os.path.join(ROCM, "include", "hip", "hip_runtime.h")):
+        pytest.skip("needs g++ and the HIP headers")
+    src, exe = tmp_path / "small.cpp", str(tmp_path / "small")
+    src.write_text(SMALL)
+    r = subprocess.run([gxx, "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+                        "-D__HIP_PLATFORM_AMD__", f"-I{ROCM}/include", f"-I{ROOT}/include", f"-I{CSRC}", str(src),
+                        os.path.join(CSRC, "attn_plan.cpp"), "-o", exe], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-3000:]
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr
