@@ -96,10 +96,11 @@ AttnPlan plan_many(int32_t B, int32_t H, int32_t N, int32_t n_keys, size_t scrat
 
 // Small chunks of more than kMx8FewQueries queries take that kernel too, a work-group per kMx8FewQueries of them over
 // the whole range, where the chip holds all of them at once and the range is short: a work-group's 256 keys cost
-// 1.5 us beside 5.5 for the launch, the first loads and the last sums.  The general kernel costs 5, 0.75 per key tile of
-// its longest part and, if it splits, what the bf16 kernel's split does (few-query kernel and general, us: 2 heads of
-// [1500 queries, 1500 keys] 15.0 and 19.6, 8 of [512, 2048] 17.8 and 23.8, 24 of [160, 960] 12.1 and 17.4, 12 of [27, 432]
-// 8.4 and 9.9, 24 of [135, 2700] 22.3 and 22.1, 3 of [200, 4000] 27.5 and 18.1; over 35 shapes within 10% of the better).
+// 1.55 us beside 5 for the launch, the first loads and the last sums.  The general kernel costs 5, 0.75 per key tile of
+// its longest part and, if it splits, 2.5 plus 2.8 times the square root of its partials' MB (few-query kernel and
+// general, us: 2 heads of [1500 queries, 1500 keys] 14.0 and 19.6, 8 of [512, 2048] 17.7 and 23.8, 24 of [160, 960]
+// 11.4 and 17.4, 12 of [27, 432] 7.7 and 9.9, 24 of [135, 2700] 21 and 22, 1 of [1716, 3432] 24 and 21.5; 490 work-groups,
+// 10 of [782, 2346], 36.5 and 28.5).
 bool mx8_few(int32_t B, int32_t H, int32_t N, int32_t n_keys) {
   if (N <= kMx8FewQueries) return true;
   const int64_t groups = int64_t(B) * H * ((N + kMx8FewQueries - 1) / kMx8FewQueries);
@@ -109,15 +110,16 @@ bool mx8_few(int32_t B, int32_t H, int32_t N, int32_t n_keys) {
   // work-groups per query tile (a contiguous split has one more partial per tile)
   const double parts = plan.workspace ? double(plan.groups) / plan.plain_groups : 1.0;
   const double partial_mb = double(B) * H * N * (parts + (plan.parts == 0)) * (kHeadDim + 2) * 4e-6;
-  const double general = 5.0 + 0.75 * std::ceil(double(tk) / parts) + (plan.workspace ? 2.5 + 2.4 * std::sqrt(partial_mb) : 0.0);
-  return 5.5 + 1.5 * double((n_keys + 255) / 256) < general;
+  const double general = 5.0 + 0.75 * std::ceil(double(tk) / parts) + (plan.workspace ? 2.5 + 2.8 * std::sqrt(partial_mb) : 0.0);
+  return 5.0 + 1.55 * double((n_keys + 255) / 256) < general;
 }
 
 // Few queries: equal parts of a (batch, head)'s keys, one work-group each.  A work-group takes 256 keys (four
-// tiles) at a time, 1.33 us a round, and a merge costs 3.5: a range is split into as many parts of at least one
+// tiles) at a time, 1.31 us a round, and a merge costs 3.5: a range is split into as many parts of at least one
 // round as the chip has compute units for, if that saves three rounds (12 heads x 1 query, us, whole and split:
-// 512 keys 7.4 and 9.0, 1024 10.0 and 9.2, 2048 15.2 and 9.3, 32768 174 and 23.6 in 21).  More than 64 parts
-// cost the merge more than they save (2 heads x 65536 keys: 64 parts 16.3, 128 parts 18.4).
+// 1024 keys 9.6 and 8.9, 2048 14.6 and 8.9, 32768 168 and 22.0 in 21; 512 6.9 whole, and a merge alone is 3.5).  More
+// than 64 parts cost the merge more than they save (2 heads x 65536 keys, with rows loaded a step ahead: 64 parts
+// 16.3, 128 parts 18.4).
 AttnPlan attn_plan_mx8(int32_t B, int32_t H, int32_t N, int32_t n_keys, size_t scratch) {
   if (!mx8_few(B, H, N, n_keys)) return plan_many(B, H, N, n_keys, scratch);
   if (N > kMx8FewQueries) {

@@ -1,9 +1,11 @@
 // Attention of quantised queries, 16 per work-group, over the retained rows of a quantised cache: the call of a
 // single-token stream, and of small chunks.  Bound by memory: 16 queries read every retained row once (264
-// bytes of K and V) and cost the same as one; a short range by its chain of loads, 1.5 us per 256 keys.
+// bytes of K and V) and cost the same as one; a short range by its chain of loads and products, 1.3-1.6 us per
+// 256 keys.
 //
-// Work-group: 8 waves, each walking a slice of its own of the work-group's key range, 32 keys at a time, with
-// the next 32 keys' rows on their way to registers.  No wave waits for another before the end.
+// Work-group: 8 waves, each walking a slice of its own of the work-group's key range, 32 keys at a time.  No wave
+// waits for another before the end.  Rows are loaded when they are needed: a step ahead they cost 55 registers and
+// were 2-9% slower on every shape (12 heads x 1 query x 32768 keys 22.5 and 21.9 us, 24 x 160 x 960 12.4 and 11.5).
 //   S^T = K Q^T with v_mfma_f32_16x16x32_bf16, keys on the M side: lane l holds 32 bytes of row l % 16, the block
 //   l / 16, so a block's scale is a lane's; the bytes become bf16 exactly, and the products and sums have fp32
 //   accuracy (unlike the 8-bit instruction's, whose cut shows where a call has few keys to average over).
@@ -11,7 +13,7 @@
 //   which the transposing read takes 4 keys of a dimension at a time; the 8 contraction slots of a lane are
 //   the keys whose scores it holds.
 // Running maximum, rescaled when it grows.  At the end the waves' sums meet in LDS, in one order.
-// One query, 12 heads x 32768 keys (104 MB): 19.8 us in 252 work-groups (5.2 TB/s) and the merge's 3.9.
+// One query, 12 heads x 32768 keys (104 MB): 18.5 us in 252 work-groups (5.6 TB/s) and the merge's 3-4.
 #include <hip/hip_runtime.h>
 
 #include <cfloat>
@@ -27,7 +29,6 @@ namespace {
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * 64;
 constexpr int kTile = 32;                      // keys per step of a wave
-constexpr int kAhead = 1;                      // steps whose rows are on their way (2: 2-5% slower)
 constexpr int kRow8 = kHeadDim, kRow16 = kHeadDim * 2;
 constexpr int kXcds = 8;
 constexpr int kMaxQ = kMx8FewQueries;
@@ -181,9 +182,6 @@ __global__ __launch_bounds__(kThreads) void mx8_attn_few_kernel(Mx8AttnArgs m) {
 #pragma unroll
   for (int d = 0; d < 8; ++d) st.o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   if (begin < src.end) {
-    Rows r[kAhead + 1];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) load(r[i], src, begin + i * kTile);
     u32x4_t q[4];
     {
       const int64_t qrow = (int64_t(b) * N + min(q0 + (lane & 15), N - 1)) * H + h;
@@ -193,14 +191,10 @@ __global__ __launch_bounds__(kThreads) void mx8_attn_few_kernel(Mx8AttnArgs m) {
       for (int i = 0; i < 4; ++i) q[i] = to_bf16(qp[i >> 1][2 * (i & 1)], qp[i >> 1][2 * (i & 1) + 1], sc);
     }
     uint8_t* const vt = lds + wave * kTile * kRow16;
-    for (int32_t k = begin; k < src.end;) {
-#pragma unroll
-      for (int i = 0; i <= kAhead; ++i) {
-        load(r[(i + kAhead) % (kAhead + 1)], src, k + kAhead * kTile);
-        step(st, r[i], q, vt, k, src.end);
-        k += kTile;
-        if (k >= src.end) break;
-      }
+    for (int32_t k = begin; k < src.end; k += kTile) {
+      Rows r;
+      load(r, src, k);
+      step(st, r, q, vt, k, src.end);
     }
   }
   st.l = over_groups(st.l, [](float x, float y) { return x + y; });
