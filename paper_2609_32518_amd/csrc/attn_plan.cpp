@@ -94,13 +94,31 @@ AttnPlan plan_many(int32_t B, int32_t H, int32_t N, int32_t n_keys, size_t scrat
 }
 }  // namespace
 
-// Small chunks of more than kMx8FewQueries queries take that kernel too, a work-group per kMx8FewQueries of them over
-// the whole range, where the chip holds all of them at once and the range is short: a work-group's 256 keys cost
-// 1.55 us beside 5 for the launch, the first loads and the last sums.  The general kernel costs 5, 0.75 per key tile of
-// its longest part and, if it splits, 2.5 plus 2.8 times the square root of its partials' MB (few-query kernel and
-// general, us: 2 heads of [1500 queries, 1500 keys] 14.0 and 19.6, 8 of [512, 2048] 17.7 and 23.8, 24 of [160, 960]
-// 11.4 and 17.4, 12 of [27, 432] 7.7 and 9.9, 24 of [135, 2700] 21 and 22, 1 of [1716, 3432] 24 and 21.5; 490 work-groups,
-// 10 of [782, 2346], 36.5 and 28.5).
+namespace {
+// Small chunks of more than kMx8FewQueries queries take that kernel too, work-groups of kMx8FewQueries of them, where the
+// chip holds all of them at once and that is estimated to be faster.  A work-group's 256 keys cost 1.55 us beside 5
+// for the launch, the first loads and the last sums; a range cut into parts costs 2.5 plus 2.8 times the square root of
+// its partials' MB, in either kernel; the general kernel costs 5 and 0.75 per key tile of its longest part.  It needs
+// more parts to fill the chip, so few heads of short ranges gain most (few-query kernel and general, us: 4 heads of
+// [256 queries, 4096 keys] 15.4 and 19.9, 1 of [756, 4536] 15.1 and 19.5, 2 of [1500, 1500] whole 14.0 and 19.6, 24
+// of [160, 960] whole 11.4 and 17.4, 12 of [27, 432] whole 7.7 and 9.9; 24 of [135, 2700] 20.2 and 22.0, 8 of [203, 9947]
+// 35.1 and 24.6; 490 work-groups, 10 of [782, 2346], 36.5 and 28.5; over 60 shapes within 10% of the better).
+struct FewPlan {
+  int32_t parts;
+  double us;
+};
+FewPlan few_plan(int32_t B, int32_t H, int32_t N, int32_t n_keys, int64_t most_parts) {
+  const int64_t rounds = (int64_t(n_keys) + 255) / 256;
+  FewPlan best{1, 5.0 + 1.55 * double(rounds)};
+  for (int64_t p = 2; p <= std::min(most_parts, rounds); p += p < 8 ? 1 : p / 4) {
+    const double mb = double(B) * H * N * double(p) * (kHeadDim + 2) * 4e-6;
+    const double us = 5.0 + 1.55 * double((rounds + p - 1) / p) + 2.5 + 2.8 * std::sqrt(mb);
+    if (us < best.us) best = FewPlan{int32_t(p), us};
+  }
+  return best;
+}
+}  // namespace
+
 bool mx8_few(int32_t B, int32_t H, int32_t N, int32_t n_keys) {
   if (N <= kMx8FewQueries) return true;
   const int64_t groups = int64_t(B) * H * ((N + kMx8FewQueries - 1) / kMx8FewQueries);
@@ -111,7 +129,7 @@ bool mx8_few(int32_t B, int32_t H, int32_t N, int32_t n_keys) {
   const double parts = plan.workspace ? double(plan.groups) / plan.plain_groups : 1.0;
   const double partial_mb = double(B) * H * N * (parts + (plan.parts == 0)) * (kHeadDim + 2) * 4e-6;
   const double general = 5.0 + 0.75 * std::ceil(double(tk) / parts) + (plan.workspace ? 2.5 + 2.8 * std::sqrt(partial_mb) : 0.0);
-  return 5.0 + 1.55 * double((n_keys + 255) / 256) < general;
+  return few_plan(B, H, N, n_keys, kAttnMaxGroups / groups).us < general;
 }
 
 // Few queries: equal parts of a (batch, head)'s keys, one work-group each.  A work-group takes 256 keys (four
@@ -123,8 +141,13 @@ bool mx8_few(int32_t B, int32_t H, int32_t N, int32_t n_keys) {
 AttnPlan attn_plan_mx8(int32_t B, int32_t H, int32_t N, int32_t n_keys, size_t scratch) {
   if (!mx8_few(B, H, N, n_keys)) return plan_many(B, H, N, n_keys, scratch);
   if (N > kMx8FewQueries) {
-    const int32_t groups = B * H * ((N + kMx8FewQueries - 1) / kMx8FewQueries);
-    return AttnPlan{groups, 0, groups, 0, 1};
+    const int64_t groups = int64_t(B) * H * ((N + kMx8FewQueries - 1) / kMx8FewQueries);
+    const int64_t tiles = int64_t(B) * H * ((N + kAttnBlockQ - 1) / kAttnBlockQ);
+    const int64_t fit = std::min<int64_t>(kAttnMaxGroups, int64_t(scratch / attn_workspace_bytes(1))) / tiles;
+    const int64_t p = few_plan(B, H, N, n_keys, std::min(fit, kAttnMaxGroups / groups)).parts;
+    if (p == 1) return AttnPlan{int32_t(groups), 0, int32_t(groups), 0, 1};
+    return AttnPlan{int32_t(groups * p), attn_workspace_bytes(int32_t(tiles * p)), int32_t(groups),
+                    size_t(tiles * p) * 2 * kAttnBlockQ * kHeadDim, int32_t(p)};
   }
   constexpr int64_t kRound = 4, kMostParts = 64, kWorthRounds = 3;
   const int64_t heads = int64_t(B) * H, tk = (n_keys + kAttnBlockK - 1) / kAttnBlockK;

@@ -194,7 +194,7 @@ struct Mx8AttnArgs {
   const uint8_t *v8, *v_scale;
 };
 hipError_t launch_mx8_attn(const Mx8AttnArgs& a, hipStream_t stream);
-// Its kernel of kMx8FewQueries queries per work-group (a.parts work-groups where that is all of a (batch, head)'s).
+// Its kernel of kMx8FewQueries queries per work-group, a.parts work-groups each.
 hipError_t launch_mx8_attn_few(const Mx8AttnArgs& a, hipStream_t stream);
 
 // The allocation-free entry point's scratch on the current device: a static device array of

@@ -508,9 +508,10 @@ __global__ __launch_bounds__(kThreads) void mx8_attn_kernel(Mx8AttnArgs m) {
 hipError_t launch_mx8_attn(const Mx8AttnArgs& m, hipStream_t stream) {
   if (mx8_few(m.a.B, m.a.H, m.a.N, m.a.n_keys)) {
     const hipError_t e = launch_mx8_attn_few(m, stream);
+    if (e != hipSuccess || m.a.N > kMx8FewQueries) return e == hipSuccess ? launch_attn_combine(m.a, stream) : e;
     // few rows leave the chip to the slices: as many as leave each one batch of partials, loaded together
     const int32_t p = m.a.parts;
-    return e == hipSuccess ? launch_attn_combine(m.a, stream, p > 16 ? 8 : p > 8 ? 4 : p > 4 ? 2 : 1) : e;
+    return launch_attn_combine(m.a, stream, p > 16 ? 8 : p > 8 ? 4 : p > 4 ? 2 : 1);
   }
   if (m.a.parts)
     hipLaunchKernelGGL(mx8_attn_kernel<true>, dim3(unsigned(m.a.groups)), dim3(kThreads), 0, stream, m);

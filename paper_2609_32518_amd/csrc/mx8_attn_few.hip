@@ -162,7 +162,7 @@ __global__ __launch_bounds__(kThreads) void mx8_attn_few_kernel(Mx8AttnArgs m) {
   const AttnArgs& a = m.a;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int32_t N = a.N, H = a.H, G = gridDim.x, tiles = (N + kMaxQ - 1) / kMaxQ;   // several only where a.parts is 1
+  const int32_t N = a.N, H = a.H, G = gridDim.x, tiles = (N + kMaxQ - 1) / kMaxQ;
   // as in the general kernel: an XCD's work-groups are consecutive, so that a head's query tiles share its L2
   const int32_t xcd = blockIdx.x % kXcds;
   const int32_t grp = xcd * (G / kXcds) + min(xcd, G % kXcds) + blockIdx.x / kXcds;
@@ -235,7 +235,9 @@ __global__ __launch_bounds__(kThreads) void mx8_attn_few_kernel(Mx8AttnArgs m) {
       *reinterpret_cast<bf16x4_t*>(a.out + ((int64_t(b) * N + q0 + n) * H + h) * kHeadDim + 4 * d4) = v;
       if (a.lse && d4 == 0) a.lse[(int64_t(b) * H + h) * N + q0 + n] = mm * a.scale + logf(l);
     } else {
-      const int64_t prow = int64_t(grp) * 2 * kAttnBlockQ + n;
+      // the merge's layout: a work-group's partials per 256-query tile and part
+      const int32_t tile = bh * ((N + kAttnBlockQ - 1) / kAttnBlockQ) + q0 / kAttnBlockQ;
+      const int64_t prow = (int64_t(tile) * a.parts + (grp - int32_t(sg.t) * a.parts)) * 2 * kAttnBlockQ + q0 % kAttnBlockQ + n;
       *reinterpret_cast<f32x4_t*>(a.part_o + prow * kHeadDim + 4 * d4) = o;
       if (d4 == 0) {
         a.part_ml[prow * 2] = mm;

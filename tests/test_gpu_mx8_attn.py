@@ -131,7 +131,8 @@ def test_every_element(shape):
 # wave, and the first sizes past those (the general kernel)
 SMALL = [(3, 3, 1, 18, 0, 23, 22, 1, 22), (2, 5, 3, 7, 2, 9, 30, 1, 8), (1, 2, 17, 23, 1, 4, 9, 1, 3), (1, 24, 1, 33, 0, 6, 5, 2, 4),
          (1, 15, 7, 37, 0, 3, 2, 1, 0), (2, 1, 30, 52, 0, 2, 1, 1, 0), (1, 12, 1, 17, 0, 30, 29, 1, 29), (1, 7, 17, 17, 1, 5, 14, 2, 3),
-         (1, 2, 16, 20, 0, 12, 30, 2, 9)]
+         (1, 2, 16, 20, 0, 12, 30, 2, 9),
+         (1, 1, 28, 27, 1, 6, 12, 1, 4), (2, 3, 1, 259, 0, 9, 8, 1, 8), (1, 4, 16, 16, 0, 17, 16, 1, 16), (1, 5, 1, 20, 2, 300, 400, 1, 250)]
 
 
 @pytest.mark.parametrize("shape", SMALL)

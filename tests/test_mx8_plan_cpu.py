@@ -121,19 +121,28 @@ using namespace unstep;
 #define CHECK(x) do { if (!(x)) { std::printf("line %d: %s\n", __LINE__, #x); return 1; } } while (0)
 int main() {
   srand(2);
-  int small = 0;
+  int small = 0, cut = 0;
   for (int i = 0; i < 50000; ++i) {
     const int B = 1 + rand() % 3, H = 1 + rand() % 60, N = 17 + rand() % (1 << (3 + rand() % 10));
     const int keys = 1 + rand() % (1 << (4 + rand() % 13));
     if (!mx8_few(B, H, N, keys)) continue;
     ++small;
     const int tiles = (N + kMx8FewQueries - 1) / kMx8FewQueries;
-    for (size_t scratch : {size_t(0), size_t(kAttnMaxWorkspace)}) {
+    const int tiles256 = (N + kAttnBlockQ - 1) / kAttnBlockQ, tk = (keys + kAttnBlockK - 1) / kAttnBlockK;
+    for (size_t scratch : {size_t(0), size_t(kAttnMaxWorkspace), attn_workspace_bytes(rand() % 256)}) {
       const AttnPlan p = attn_plan_mx8(B, H, N, keys, scratch);
-      CHECK(p.workspace == 0 && p.parts == 1 && p.groups == B * H * tiles && p.plain_groups == p.groups && p.groups <= kAttnMaxGroups);
+      CHECK(p.plain_groups == B * H * tiles && p.parts >= 1 && p.parts <= tk && p.groups == p.plain_groups * p.parts);
+      CHECK(p.groups <= kAttnMaxGroups && p.workspace <= scratch);
+      if (p.parts == 1) {
+        CHECK(p.workspace == 0);
+        continue;
+      }
+      ++cut;
+      CHECK(p.workspace == attn_workspace_bytes(B * H * tiles256 * p.parts));
+      CHECK(p.part_o_floats == size_t(B) * H * tiles256 * p.parts * 2 * kAttnBlockQ * kHeadDim);
     }
   }
-  CHECK(small > 1000);
+  CHECK(small > 1000 && cut > 1000);
   CHECK(mx8_few(1, 1, 1, 1) && mx8_few(4, 400, 16, 1 << 20));          // up to 16 queries always
   CHECK(mx8_few(1, 12, 27, 432) && mx8_few(1, 8, 512, 2048));
   CHECK(!mx8_few(1, 12, 17, 18720) && !mx8_few(1, 12, 4680, 18720) && !mx8_few(1, 60, 32, 19200) && !mx8_few(1, 257, 17, 64));
