@@ -39,12 +39,14 @@ typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef short i16x4_t __attribute__((ext_vector_type(4)));
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) i16x4_t lds_i16x4_t;
 typedef __attribute__((address_space(3))) u32x4_t lds_u32x4_t;
 typedef __attribute__((address_space(3))) uint32_t lds_u32_t;
+typedef __attribute__((address_space(3))) f32x4_t lds_f32x4_t;
 typedef __attribute__((address_space(3))) bf16x4_t lds_bf16x4_t;
 typedef __attribute__((address_space(3))) void lds_void_t;
 
@@ -97,6 +99,9 @@ constexpr int kLdsV = kRing * kTile8, kLdsS = kLdsV + kRing * kTile16,
 // output staging of a finished query tile in the rings: 272-byte rows
 constexpr int kOutPitch = kRow16 + 16;
 static_assert(kBlockQ * kOutPitch <= kLdsBytes, "the output tile must fit the rings");
+// ... and of its partials, half a tile at a time: 528-byte rows, kRowsAtOnce of them by all threads
+constexpr int kHalfQ = kBlockQ / 2, kPartRow = kHeadDim * 4, kPartPitch = kPartRow + 16, kRowsAtOnce = kThreads / 32;
+static_assert(kHalfQ * kPartPitch <= kLdsBytes && kHalfQ * 2 == kBlockQ, "half the partials must fit the rings");
 constexpr int kFetchAhead = 4;               // fragments read ahead of the product that uses them
 
 struct Walk {
@@ -484,20 +489,52 @@ __global__ __launch_bounds__(kThreads) void mx8_attn_kernel(Mx8AttnArgs m) {
         if (qs < N) *reinterpret_cast<u32x4_t*>(a.out + ((int64_t(b) * N + qs) * H + h) * kHeadDim + 8 * pc) = v;
       }
       if (qi < N && a.lse && half == 0) a.lse[(int64_t(b) * H + h) * N + qi] = off * a.scale + logf(l_tot);
-    } else if (qi < N) {
-      const int64_t prow = (int64_t(g) * 2 + sg.slot) * kBlockQ + r;
+    } else {
       const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
-      float* op = a.part_o + prow * kHeadDim + 4 * half;
+      const int64_t prow0 = (int64_t(g) * 2 + sg.slot) * kBlockQ;
+      if (qi < N && half == 0) {
+        a.part_ml[(prow0 + r) * 2] = l_tot > 0.f ? off : -INFINITY;
+        a.part_ml[(prow0 + r) * 2 + 1] = l_tot;
+      }
+      // partials of a tile with queries of both groups leave through the rings as whole rows, A's and then B's; those
+      // of few queries, or of a contiguous split's two ends, from where they are, 32 bytes of 32 rows at a time
+      // (us, through the rings and not: 10 heads of [782 queries, 4692 keys] 30.3 and 31.9, 24 of [390, 3120] 27.5 and
+      // 28.8, 6 of [1568, 29792] 106.6 and 108.5; 130 of [20, 1600] in a contiguous split 39.3 and 23.6)
+      if (!kParts || qt * kBlockQ + kHalfQ >= N) {
+        if (qi < N) {
+          float* op = a.part_o + (prow0 + r) * kHeadDim + 4 * half;
 #pragma unroll
-      for (int d = 0; d < 4; ++d)
+          for (int d = 0; d < 4; ++d)
 #pragma unroll
-        for (int gg = 0; gg < 4; ++gg)
-          *reinterpret_cast<float4*>(op + d * 32 + 8 * gg) =
-              make_float4(acc.o[d][4 * gg] * inv, acc.o[d][4 * gg + 1] * inv, acc.o[d][4 * gg + 2] * inv,
-                          acc.o[d][4 * gg + 3] * inv);
-      if (half == 0) {
-        a.part_ml[prow * 2] = l_tot > 0.f ? off : -INFINITY;
-        a.part_ml[prow * 2 + 1] = l_tot;
+            for (int gg = 0; gg < 4; ++gg)
+              *reinterpret_cast<float4*>(op + d * 32 + 8 * gg) =
+                  make_float4(acc.o[d][4 * gg] * inv, acc.o[d][4 * gg + 1] * inv, acc.o[d][4 * gg + 2] * inv,
+                              acc.o[d][4 * gg + 3] * inv);
+        }
+      } else {
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+          barrier();
+          if (group == part) {
+            const uint32_t orow = lds0 + uint32_t((r % kHalfQ) * kPartPitch + 16 * half);
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+              for (int gg = 0; gg < 4; ++gg)
+                *reinterpret_cast<lds_f32x4_t*>(uintptr_t(orow + (d * 32 + 8 * gg) * 4)) =
+                    f32x4_t{acc.o[d][4 * gg] * inv, acc.o[d][4 * gg + 1] * inv, acc.o[d][4 * gg + 2] * inv, acc.o[d][4 * gg + 3] * inv};
+          }
+          barrier();
+          const int pc = tid & 31;
+#pragma unroll
+          for (int i = 0; i < kHalfQ / kRowsAtOnce; ++i) {
+            // every work-group from another row on: the partials lie 256 KB apart, and 256 work-groups that write the
+            // same rows at once meet in the same memory channels (35.2 us instead of 33.5 for 8 heads of [1024, 4096])
+            const int rs = (tid >> 5) + kRowsAtOnce * ((i + g) % (kHalfQ / kRowsAtOnce)), rt = kHalfQ * part + rs;
+            const f32x4_t v = *reinterpret_cast<const lds_f32x4_t*>(uintptr_t(lds0 + uint32_t(rs * kPartPitch + pc * 16)));
+            if (qt * kBlockQ + rt < N) *reinterpret_cast<f32x4_t*>(a.part_o + (prow0 + rt) * kHeadDim + 4 * pc) = v;
+          }
+        }
       }
     }
   } while (!kParts && u_hi > u_begin);
