@@ -337,8 +337,9 @@ int unstep_kv_append_mx8(unstep_cache* c, int32_t start_frame, int32_t n_frames,
  * keys, for q8, q_scale as unstep_kv_append_mx8 writes them.  Products of e4m3 values with fp32
  * accumulation (the matrix instruction cuts a product below 2^-13 of the largest of its 16 dimensions, so
  * a score that one product of size P dominates is off by up to 2^-8 P), fp32 softmax, probabilities rounded
- * to bf16 for their product with the values; out is bf16 [batch, N, n_heads, 128], lse (optional) float
- * [batch, n_heads, N], the natural logarithm of the sum.
+ * to bf16 for their product with the values (a call without lse may divide by the sum of the rounded ones, so
+ * out can differ in its last bits); out is bf16 [batch, N, n_heads, 128], lse (optional) float [batch, n_heads, N],
+ * the natural logarithm of the sum.
  * Scale bytes must lie in [1, 254].  A score that overflows to -infinity weighs nothing; a NaN, or nothing but
  * such scores, makes the query's output NaN.  Workspace: as unstep_window_attn, of unstep_attn_workspace_size bytes
  * for this handle.  Errors: those of unstep_window_attn, plus E_NULL (q_scale), E_STATE (the cache holds bf16 rows). */

@@ -89,6 +89,15 @@ __device__ __forceinline__ i32x8_t join(u32x4_t a, u32x4_t b) {
 // A's M phase u, and overwriting K(u-3), last read one phase before group A's write.  V tiles: ring of
 // three, V(u) written in V phase u - 1 and read in M phase u + 1.  One barrier per phase.
 //
+// The row sums of a call without a log-sum are four 16x16x32 products a tile, of P^T as it lies in the registers: its
+// lanes are 16 columns of 32 rows there, keys 0..7 and 8..15 of queries 0..15 in lanes 0..15 and 32..47, those of
+// queries 16..31 in the others, so a row of ones for the first and one for the second pick both sums.  They are the
+// sums of the rounded weights, whose rounding then cancels where few keys hold a row (error against float64 of a step
+// with scores of tens 0.0022 instead of 0.0024-0.0025), and cost less than 32 additions (359 us instead of 362 for
+// 4680 queries x 18720 keys x 12 heads).  A log-sum needs the weights before their rounding, and both take 2.5% longer.
+// A product spreads a NaN or infinity of one query to the one 16 on: such a sum sends the work-group through its range
+// again, with additions.
+//
 // The exponent offset m is the row's maximum over the range's first tile and enters the product as its
 // accumulator, so a score costs one exp2, one add and half a conversion; a row whose sum passes 2^64
 // makes the work-group redo its range with the exact maximum.
@@ -132,7 +141,9 @@ struct Acc {
   f32x16_t s[2];               // S^T of the current tile: keys 32 kb .. 32 kb + 31
   bf16x8_t p[2][2];            // P^T of the previous tile: (key block, 16-key step)
   f32x16_t negm;               // - exponent offset, in every element
-  float l;                     // row sum (this lane's half of the keys)
+  float l;                     // row sum (this lane's half of the keys, or half the sum)
+  f32x4_t sum;                 // sums by products: element 0 query lane, 1 query 16 + lane, in lanes 0..15
+  bf16x8_t pick;               // ... and the rows that pick them
   float mx;                    // running row max (max-only walk)
 };
 
@@ -196,11 +207,13 @@ __device__ __forceinline__ Frag fetch(int j, int kslot, int vslot, const Walk& w
   return f;
 }
 
-template <bool kZero>
+template <bool kZero, bool kSum>
 __device__ __forceinline__ void run(Acc& a, int j, const Frag& f, const uint32_t (&ks)[2], const Queries& q) {
   if (j < 16) {
     a.o[j & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, f.r[0]), a.p[j >> 3][(j >> 2) & 1],
                                                          a.o[j & 3], 0, 0, 0);
+    if (kSum && (j & 3) == 0)
+      a.sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.pick, a.p[j >> 3][(j >> 2) & 1], a.sum, 0, 0, 0);
   } else {
     const int kb = (j - 16) >> 1;
     const f32x16_t zero = {};
@@ -218,20 +231,20 @@ __device__ __forceinline__ constexpr int jobs() { return kPart == 0 ? 20 : kPart
 template <int kPart>
 __device__ __forceinline__ constexpr int job_at(int i) { return kPart == 0 ? job_id(i) : kPart == 1 ? 16 + i : i; }
 
-template <int kPart, bool kZero, int J>
+template <int kPart, bool kZero, bool kSum, int J>
 struct MJob {
   static __device__ __forceinline__ void go(Acc& a, Frag (&f)[jobs<kPart>()], int kslot, int vslot, const uint32_t (&ks)[2],
                                             const Queries& q, const Walk& w) {
     constexpr int kNext = J + kFetchAhead;
     if constexpr (kNext < jobs<kPart>()) f[kNext] = fetch(job_at<kPart>(kNext), kslot, vslot, w);
-    run<kZero>(a, job_at<kPart>(J), f[J], ks, q);
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    run<kZero, kSum>(a, job_at<kPart>(J), f[J], ks, q);
+    __builtin_amdgcn_sched_group_barrier(0x008, kSum && job_at<kPart>(J) < 16 && (job_at<kPart>(J) & 3) == 0 ? 2 : 1, 0);
     if constexpr (kNext < jobs<kPart>()) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-    if constexpr (J + 1 < jobs<kPart>()) MJob<kPart, kZero, J + 1>::go(a, f, kslot, vslot, ks, q, w);
+    if constexpr (J + 1 < jobs<kPart>()) MJob<kPart, kZero, kSum, J + 1>::go(a, f, kslot, vslot, ks, q, w);
   }
 };
 
-template <int kPart, bool kZero>
+template <int kPart, bool kZero, bool kSum>
 __device__ __forceinline__ void m_phase(Acc& a, int kslot, int vslot, const Queries& q, const Walk& w) {
   Frag f[jobs<kPart>()];
   uint32_t ks[2] = {0, 0};
@@ -243,11 +256,12 @@ __device__ __forceinline__ void m_phase(Acc& a, int kslot, int vslot, const Quer
 #pragma unroll
   for (int i = 0; i < kFetchAhead; ++i) f[i] = fetch(job_at<kPart>(i), kslot, vslot, w);
   __builtin_amdgcn_sched_group_barrier(0x100, 2 * kFetchAhead + (kPart != 2 ? 2 : 0), 0);
-  MJob<kPart, kZero, 0>::go(a, f, kslot, vslot, ks, q, w);
+  MJob<kPart, kZero, kSum, 0>::go(a, f, kslot, vslot, ks, q, w);
   // the products stay in this phase: their results are first used after the barrier, past which the compiler
   // would otherwise move them, into the other wave's multiplying phase
   if (kPart != 2) asm volatile("" : "+v"(a.s[0]), "+v"(a.s[1]));
   if (kPart != 1) asm volatile("" : "+v"(a.o[0]), "+v"(a.o[1]), "+v"(a.o[2]), "+v"(a.o[3]));
+  if (kPart != 1 && kSum) asm volatile("" : "+v"(a.sum));
 }
 
 // V phase of tile t (kSlot = t % 3).  kMode 0: offsets from the first tile; 1: offsets given; 2: row max only.
@@ -255,7 +269,7 @@ __device__ __forceinline__ void m_phase(Acc& a, int kslot, int vslot, const Quer
 // V(t + 1) into that of V(t - 2)), K(t + 3) and V(t + 2) start; past the range's end it repeats the last
 // tile, whose copies nothing reads.  It runs between quarters of the softmax, so that the four waves of a phase do
 // not queue at the memory pipelines at once.
-template <int kMode, int kSlot, bool kOneRun, bool kIdle, bool kFirst>
+template <int kMode, int kSlot, bool kSum, bool kOneRun, bool kIdle, bool kFirst>
 __device__ __forceinline__ void v_phase(Acc& a, Stage& st, Walk& w, int32_t t) {
   if (kIdle) {
     store_k(st, w, (kSlot + 2) % kRing);
@@ -299,23 +313,25 @@ __device__ __forceinline__ void v_phase(Acc& a, Stage& st, Walk& w, int32_t t) {
         const int kb = q >> 1, i = 8 * (q & 1) + e;
         const float e0 = __builtin_amdgcn_exp2f(a.s[kb][i]);
         const float e1 = __builtin_amdgcn_exp2f(a.s[kb][i + 1]);
-        acc0 += e0;
-        acc1 += e1;
+        if (!kSum) {
+          acc0 += e0;
+          acc1 += e1;
+        }
         a.p[kb][i >> 3][i & 7] = (__bf16)e0;
         a.p[kb][i >> 3][(i & 7) + 1] = (__bf16)e1;
       }
     }
     __builtin_amdgcn_sched_barrier(0);
   }
-  a.l += acc0 + acc1;
+  if (!kSum) a.l += acc0 + acc1;
 }
 
-template <int kMode, int kSlot, bool kOneRun, bool kIdle, bool kFirst = false>
+template <int kMode, int kSlot, bool kSum, bool kOneRun, bool kIdle, bool kFirst = false>
 __device__ __forceinline__ void step(Acc& a, Stage& st, Walk& w, const Queries& q, int32_t t) {
   if (t >= w.n) return;
-  if (!kIdle) m_phase<kFirst ? 1 : 0, (kFirst && kMode == 0) || kMode == 2>(a, kSlot, (kSlot + 2) % kRing, q, w);
+  if (!kIdle) m_phase<kFirst ? 1 : 0, (kFirst && kMode == 0) || kMode == 2, kSum>(a, kSlot, (kSlot + 2) % kRing, q, w);
   barrier();
-  v_phase<kMode, kSlot, kOneRun, kIdle, kFirst>(a, st, w, t);
+  v_phase<kMode, kSlot, kSum, kOneRun, kIdle, kFirst>(a, st, w, t);
   barrier();
 }
 
@@ -341,22 +357,34 @@ __device__ __forceinline__ void walk_fill(const Start& b, const Walk& w) {
   store_k(b.second, w, 1);
 }
 
-template <int kMode, bool kOneRun, bool kIdle>
+// kSum: the row sums by products with rows of ones and zeros, of the rounded weights (mode 0).
+template <int kMode, bool kSum, bool kOneRun, bool kIdle>
 __device__ __forceinline__ void walk(Acc& a, Stage& st, Walk& w, const Queries& q, int group) {
   const f32x16_t zero = {};
 #pragma unroll
   for (int d = 0; d < 4; ++d) a.o[d] = zero;
   a.l = 0.f;
   a.mx = -INFINITY;
+  if (kSum) {
+    const int row = threadIdx.x & 15;
+    const uint32_t one = row < 2 && ((threadIdx.x >> 4) & 1) == row ? 0x3f803f80u : 0u;
+    a.pick = __builtin_bit_cast(bf16x8_t, u32x4_t{one, one, one, one});
+    a.sum = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
   barrier();                                   // the first slots are complete: global phase 0
   if (group == 1) barrier();                   // group B idles in phase 0
-  step<kMode, 0, kOneRun, kIdle, true>(a, st, w, q, 0);
+  step<kMode, 0, kSum, kOneRun, kIdle, true>(a, st, w, q, 0);
   for (int32_t t0 = 1; t0 < w.n; t0 += kRing) {
-    step<kMode, 1, kOneRun, kIdle>(a, st, w, q, t0);
-    step<kMode, 2, kOneRun, kIdle>(a, st, w, q, t0 + 1);
-    step<kMode, 0, kOneRun, kIdle>(a, st, w, q, t0 + 2);
+    step<kMode, 1, kSum, kOneRun, kIdle>(a, st, w, q, t0);
+    step<kMode, 2, kSum, kOneRun, kIdle>(a, st, w, q, t0 + 1);
+    step<kMode, 0, kSum, kOneRun, kIdle>(a, st, w, q, t0 + 2);
   }
-  if (!kIdle && kMode != 2) m_phase<2, false>(a, 0, (w.n - 1) % kRing, q, w);
+  if (!kIdle && kMode != 2) m_phase<2, false, kSum>(a, 0, (w.n - 1) % kRing, q, w);
+  if (!kIdle && kSum) {
+    const int col = threadIdx.x & 31;
+    const float low = __shfl(a.sum[0], col & 15), high = __shfl(a.sum[1], col & 15);
+    a.l = 0.5f * (col < 16 ? low : high);
+  }
   barrier();
   if (group == 0) barrier();                   // group A idles in the last phase
 }
@@ -368,17 +396,17 @@ __device__ __forceinline__ void walk_again(Acc& a, Stage& st, Walk& w, const Que
   Start b;
   walk_load<false>(b, st, w);
   walk_fill(b, w);
-  walk<2, false, kIdle>(a, st, w, q, group);
+  walk<2, false, false, kIdle>(a, st, w, q, group);
   const float m = fmaxf(fmaxf(a.mx, __shfl_xor(a.mx, 32)), -FLT_MAX);
 #pragma unroll
   for (int i = 0; i < 16; ++i) a.negm[i] = -m;
   walk_load<false>(b, st, w);
   walk_fill(b, w);
-  walk<1, false, kIdle>(a, st, w, q, group);
+  walk<1, false, false, kIdle>(a, st, w, q, group);
 }
 
-// kParts: a whole number of work-groups per query tile (a.parts), one segment each.
-template <bool kParts>
+// kParts: a whole number of work-groups per query tile (a.parts), one segment each.  kSum: as in walk().
+template <bool kParts, bool kSum>
 __global__ __launch_bounds__(kThreads) void mx8_attn_kernel(Mx8AttnArgs m) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kLdsBytes];
   const AttnArgs& a = m.a;
@@ -458,9 +486,9 @@ __global__ __launch_bounds__(kThreads) void mx8_attn_kernel(Mx8AttnArgs m) {
     // a wave whose 32 queries all lie past the chunk's end runs the loads and barriers only
     const bool idle = qt * kBlockQ + wave * 32 >= N;
     if (one_run)
-      idle ? walk<0, true, true>(acc, st, w, q, group) : walk<0, true, false>(acc, st, w, q, group);
+      idle ? walk<0, kSum, true, true>(acc, st, w, q, group) : walk<0, kSum, true, false>(acc, st, w, q, group);
     else
-      idle ? walk<0, false, true>(acc, st, w, q, group) : walk<0, false, false>(acc, st, w, q, group);
+      idle ? walk<0, kSum, false, true>(acc, st, w, q, group) : walk<0, kSum, false, false>(acc, st, w, q, group);
     if (__syncthreads_or(!idle && !(acc.l <= 0x1p64f)))
       idle ? walk_again<true>(acc, st, w, q, group) : walk_again<false>(acc, st, w, q, group);
 
@@ -550,10 +578,9 @@ hipError_t launch_mx8_attn(const Mx8AttnArgs& m, hipStream_t stream) {
     const int32_t p = m.a.parts;
     return launch_attn_combine(m.a, stream, p > 16 ? 8 : p > 8 ? 4 : p > 4 ? 2 : 1);
   }
-  if (m.a.parts)
-    hipLaunchKernelGGL(mx8_attn_kernel<true>, dim3(unsigned(m.a.groups)), dim3(kThreads), 0, stream, m);
-  else
-    hipLaunchKernelGGL(mx8_attn_kernel<false>, dim3(unsigned(m.a.groups)), dim3(kThreads), 0, stream, m);
+  const auto kernel = m.a.parts ? (m.a.lse ? mx8_attn_kernel<true, false> : mx8_attn_kernel<true, true>)
+                                : (m.a.lse ? mx8_attn_kernel<false, false> : mx8_attn_kernel<false, true>);
+  hipLaunchKernelGGL(kernel, dim3(unsigned(m.a.groups)), dim3(kThreads), 0, stream, m);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? launch_attn_combine(m.a, stream) : e;
 }

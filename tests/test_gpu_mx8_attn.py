@@ -219,6 +219,56 @@ def test_scores_that_grow_in_every_dimension(shape, sign):
         c.check(*c.run(use_split=split))
 
 
+def check_without_lse(c, want, E=0.0, **kw):
+    """A call without a log-sum may divide by the sum of the rounded weights: p (1 + d), |d| <= 2^-8, above and below,
+    so besides the output's own rounding the error is at most 2^-8 (A + |o|) (1 + 2^-7) <= 2^-7 (1 + 2^-7) A, and the
+    terms of fp32 and of the 8-bit products as above."""
+    o, _, A, top = want
+    got = bf16_to_f64(host(c.cache.unstep_window_attn_mx8(*c.a, c.q8, c.qs, **kw)))
+    bound = 2.0 ** -8 * np.abs(o) * (1 + 2.0 ** -7) + 2.0 ** -7 * (1 + 2.0 ** -6) * A + 2.0 ** -17 * A * (1 + top) + A * (4.0 ** E - 1)
+    assert np.isfinite(got).all()
+    assert (np.abs(got - o) <= bound).all(), float((np.abs(got - o) / bound).max())
+
+
+@pytest.mark.parametrize("shape", [SHAPES[i] for i in (2, 9, 11, 13, 14, 15, 17, 18, 19, 20)] + [(1, 12, 16, 31, 0, 6, 5, 1, 5)])
+def test_without_a_log_sum(shape):
+    c = Case(*shape)
+    want = c.expected()
+    for split in (True, False):
+        check_without_lse(c, want, use_split=split)
+
+
+@pytest.mark.parametrize("shape", [(1, 130, 4, 5, 0, 80, 79, 1, 79), (1, 2, 16, 20, 0, 12, 30, 2, 9)])
+def test_hard_scores_without_a_log_sum(shape):
+    """Scores that grow by hundreds; keys whose scores are -infinity; a NaN query, which leaves every other alone."""
+    c = Case(*shape, q_scale=1.0)
+    n = len(c.rows)
+    q, k = mx8.values(*c.q), mx8.values(*c.k)
+    q[..., 0], k[..., 0] = 8.0, 0.0
+    k[:, :, c.rows, 0] = np.linspace(-40, 40, n)
+    c.q, c.k = mx8.quantise(q), mx8.quantise(k)
+    c.make()
+    for split in (True, False):
+        check_without_lse(c, c.expected(), E=c.cut(), use_split=split)
+    c = Case(*shape)
+    q, k = mx8.values(*c.q), mx8.values(*c.k)
+    q[..., 0], k[..., 0] = 2.0 ** 66, 0.0
+    k[:, :, c.rows[:n // 2], 0] = -2.0 ** 66
+    c.q, c.k = mx8.quantise(q), mx8.quantise(k)
+    c.make()
+    c.rows = c.rows[n // 2:]
+    check_without_lse(c, c.expected())
+    c = Case(*shape)
+    o, _, A, top = c.expected()
+    c.q8.view(torch.uint8)[0, 3, 1, 77] = 0xFF
+    for split in (True, False):
+        out = c.cache.unstep_window_attn_mx8(*c.a, c.q8, c.qs, use_split=split)
+        assert torch.isnan(out[0, 3, 1]).all()
+        got = bf16_to_f64(host(out))
+        got[0, 3, 1] = o[0, 3, 1]
+        assert (np.abs(got - o) <= 2.0 ** -6 * A + 2.0 ** -17 * A * (1 + top)).all()
+
+
 def test_equal_keys_give_the_mean():
     c = Case(1, 2, 3, 7, 0, 6, 5, 1, 5)
     c.q = (np.zeros_like(c.q[0]), c.q[1])
